@@ -217,6 +217,15 @@ int32_t edl_init(edl_handle** out, const edl_config* cfg, uint64_t seed, void* d
  * streams.  Results do not depend on the choice, bit for bit. */
 int32_t edl_set_side_streams(edl_handle* h, void* wgrad_stream, void* update_stream);
 
+/* Dropout behind the hidden fully connected layers (after their ReLU) in the training passes of edl_step, edl_gradients and
+ * edl_profile_parallelism: MLP fc1 and fc2, VGG and AlexNet fc1 and fc2.  rate 0 (a new job's): none.  The masks are
+ * edl_dropout's with key edl_dropout_key(seed, step, the layer's place in the layer list) and the sample's place in the aggregate mini-batch
+ * as its row number: they do not depend on p, on how a mini-batch is cut into shards or passes, and a mini-batch redone
+ * before edl_apply (section 4.2's approximate recovery) has the same ones.  The state image carries the rate and
+ * edl_restore adopts it.  The debugging hooks run without dropout.  EDL_EINVAL: rate outside [0, 1), or above 0 for a model
+ * without such layers (the residual nets). */
+int32_t edl_set_dropout(edl_handle* h, float rate);
+
 /* Named integer options of the library (process-wide; see Conventions).  EDL_EINVAL for an unknown name.  Names:
  * force_tile (-1, or 0..3 = every forward / input-gradient launch on 128x128, 128x64, 128x32, 64x64 tiles),
  * wgrad_stream (1: jobs created from now on use the library's side streams; 0: they do not), wgrad_tail_main,
@@ -327,10 +336,10 @@ int32_t edl_profile_parallelism(edl_handle* h, int32_t min_p, int32_t max_p, int
  * running[R] (float32, little endian), written to device memory dev_dst of
  * capacity cap.  The header carries the job's meta-data (section 4.2): model,
  * dtype, seed, N, B, progress, optimizer and its coefficients (lr, momentum,
- * wd; beta2, eps).  edl_restore refuses (EDL_EINVAL) an image of another model,
+ * wd; beta2, eps) and the rate of edl_set_dropout.  edl_restore refuses (EDL_EINVAL) an image of another model,
  * job size, optimizer or dtype (the worker's buffers were laid out for its
- * own), and ADOPTS the rest: seed, progress and the optimizer's coefficients
- * replace what the worker was created with, so a joiner continues exactly as
+ * own), and ADOPTS the rest: seed, progress, the optimizer's coefficients and
+ * the dropout rate replace what the worker was created with, so a joiner continues exactly as
  * the job it joined.  Gradients pending from before the restore are void. */
 int32_t edl_snapshot(edl_handle* h, void* dev_dst, size_t cap, size_t* out_written);
 int32_t edl_restore(edl_handle* h, const void* dev_src, size_t len);
@@ -419,6 +428,27 @@ int32_t edl_average_update(int32_t p, const float* const* dev_grads, float* dev_
 int32_t edl_adam_update(int32_t p, const float* const* dev_grads, const float* shares, float* dev_w, float* dev_m,
                         float* dev_s, uint16_t* dev_w16, int64_t P, float lr, float beta1, float beta2, float eps,
                         float wd, int64_t t, void* hip_stream);
+
+/* ---- operators of a classifier's head on caller buffers ---------------------------------------------------------
+ * Dropout, the log probabilities of given classes, and the same straight from features and classifier weights, each with
+ * its gradient.  dtype is EDL_DTYPE_* and names the elements of matrices (bf16: raw 16 bits); vectors are float32, class
+ * numbers int32.  Matrices are row-major, `ld` elements (at most 2^31 - 1) between rows, any ld >= the row's length, aligned to their elements
+ * only; nothing between rows is read or written.  Work is queued on hip_stream (NULL: the default stream), which has to
+ * belong to the current device, as all pointers have to; nothing is allocated, nothing synchronises, and every call may be
+ * captured into a graph.  Results do not depend on anything but the arguments: no atomics, the same bits every time.
+ * Calls of no rows return EDL_OK and touch nothing. */
+
+/* y = kept ? x / (1 - rate) : 0 for a [rows][cols] matrix, rounded once; y may be x (with the same ld) and must not
+ * overlap it otherwise.  No mask is stored: whether element (r, c) is kept follows from (key, first_row + r, c) and cols
+ * alone, and the gradient of the call is the same call on the gradient of y.  Of row number R = first_row + r, columns 2i
+ * and 2i + 1 take the low and the high 32 bits of draw R * ceil(cols/2) + i of the library's generator (SplitMix64, draw j
+ * = its finaliser of key + (j+1) * 0x9E3779B97F4A7C15); an element whose 32 bits are below floor(rate * 2^32) is dropped,
+ * to +0 whatever it held.  Rows cut differently over calls (by first_row) have the same masks.  Keys of neighbouring
+ * values do not give independent masks; edl_dropout_key (host only) makes one from a seed, a step and a layer.
+ * EDL_EINVAL: rate outside [0, 1), negative sizes, bad ld or alignment; EDL_ERANGE: rows * ceil(cols/8) over 2^39. */
+int32_t edl_dropout_key(uint64_t seed, int64_t step, int32_t layer, uint64_t* out_key);
+int32_t edl_dropout(int32_t dtype, const void* dev_x, int64_t ldx, void* dev_y, int64_t ldy, int64_t rows, int64_t cols, float rate,
+                    uint64_t key, int64_t first_row, void* hip_stream);
 
 /* Measurement: with profiling on, every kernel launch of this library (any
  * handle, and the stand-alone calls) is bracketed by a HIP event pair on the

@@ -121,6 +121,10 @@ _SIGS = {
     "edl_pipeline_load": [_i64p, C.c_size_t, C.POINTER(C.c_void_p)],
     "edl_pipeline_destroy": [C.c_void_p],
     "edl_mfma_rate": [C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.POINTER(C.c_double)],
+    "edl_set_dropout": [C.c_void_p, C.c_float],
+    "edl_dropout_key": [C.c_uint64, C.c_int64, C.c_int32, C.POINTER(C.c_uint64)],
+    "edl_dropout": [C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_float, C.c_uint64,
+                    C.c_int64, C.c_void_p],
     "edl_profile": [C.c_int32],
     "edl_profile_report": [C.c_char_p, C.c_size_t, C.POINTER(C.c_size_t)],
 }
@@ -244,6 +248,89 @@ def edl_mfma_rate(dtype, blocks, iters, sink, stream=0):
 
 def edl_copy(dst, src, nbytes, stream=0):
     _check(lib.edl_copy(dst.data_ptr(), src.data_ptr(), nbytes, stream))
+
+
+# -- operators of a classifier's head ---------------------------------------------------------------------------------
+# Tensors stay where they are: matrices may be views whose rows lie any number of elements apart.  Work goes to torch's
+# current stream of the tensors' device, or to `stream` (a raw stream handle, 0 the default stream); what a call allocates
+# belongs to that stream.  Wrong arguments raise EdlError, as the library's own checks do.
+
+def _refuse(msg):
+    raise EdlError(-1, msg)
+
+
+def _dtype_of(name, x):
+    code = {"torch.float32": 0, "torch.bfloat16": 1}.get(str(x.dtype))
+    if code is None:
+        _refuse("%s must be float32 or bfloat16, not %s" % (name, x.dtype))
+    return code
+
+
+def _matrix(name, x, shape=None, like=None):
+    """(pointer, elements between rows) of a [rows][cols] tensor on a GPU."""
+    if x.dim() != 2 or (shape is not None and tuple(x.shape) != tuple(shape)):
+        _refuse("%s must be a matrix%s, not %s" % (name, "" if shape is None else " of %d x %d" % tuple(shape), tuple(x.shape)))
+    if not x.is_cuda:
+        _refuse("%s must be on a GPU" % name)
+    if like is not None and (x.dtype != like.dtype or x.device != like.device):
+        _refuse("%s is %s on %s, expected %s on %s" % (name, x.dtype, x.device, like.dtype, like.device))
+    rows, cols = x.shape
+    if cols > 1 and x.stride(1) != 1:
+        _refuse("neighbouring elements of a row of %s must be neighbours in memory" % name)
+    return x.data_ptr(), x.stride(0) if rows > 1 else cols
+
+
+def _vector(name, v, n, dtype, like):
+    """Pointer of a contiguous [n] tensor of that type on like's device; None stays None."""
+    if v is None:
+        return None
+    if str(v.dtype) != dtype or tuple(v.shape) != (n,) or v.device != like.device or not v.is_contiguous():
+        _refuse("%s must be a contiguous %s vector of %d on %s" % (name, dtype, n, like.device))
+    return v.data_ptr()
+
+
+class _On:
+    """with _On(x, stream) as raw: x's device is current and raw the stream to launch on, which torch allocates for."""
+
+    def __init__(self, x, stream):
+        import torch
+        self._guards = []
+        if torch.cuda.current_device() != x.device.index:
+            self._guards.append(torch.cuda.device(x.device))
+        if stream is not None:
+            given = torch.cuda.ExternalStream(stream, device=x.device) if stream else torch.cuda.default_stream(x.device)
+            self._guards.append(torch.cuda.stream(given))
+        self._torch, self._device = torch, x.device
+
+    def __enter__(self):
+        for g in self._guards:
+            g.__enter__()
+        return self._torch.cuda.current_stream(self._device).cuda_stream
+
+    def __exit__(self, *exc):
+        for g in reversed(self._guards):
+            g.__exit__(*exc)
+        return False
+
+
+def edl_dropout_key(seed, step, layer):
+    k = C.c_uint64()
+    _check(lib.edl_dropout_key(seed, step, layer, C.byref(k)))
+    return k.value
+
+
+def edl_dropout(x, rate, key, first_row=0, out=None, stream=None):
+    """x: [rows][cols] float32 or bfloat16; out: where the result goes (x itself: in place; None: a new tensor).
+    The gradient is the same call on the gradient of the result."""
+    dt = _dtype_of("x", x)
+    px, ldx = _matrix("x", x)
+    with _On(x, stream) as st:
+        if out is None:
+            import torch
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        py, ldy = _matrix("out", out, x.shape, x)
+        _check(lib.edl_dropout(dt, px, ldx, py, ldy, x.shape[0], x.shape[1], rate, key, first_row, st))
+    return out
 
 
 def edl_set_option(name, value):
@@ -402,6 +489,10 @@ class Job:
 
     def apply(self, p):
         _check(lib.edl_apply(self._h, p))
+
+    def set_dropout(self, rate):
+        """Dropout behind the hidden fully connected layers (MLP, VGG, AlexNet) in training passes; 0: none."""
+        _check(lib.edl_set_dropout(self._h, rate))
 
     def snapshot(self, dst=None):
         if dst is None:

@@ -14,6 +14,7 @@
 #include "graph.h"
 #include "kernels.h"
 #include "narrow.h"
+#include "operators.h"
 #include "profiler.h"
 #include "thin.h"
 #include "tune.h"
@@ -73,8 +74,10 @@ struct SnapshotHeader {
     uint32_t optimizer;
     int64_t P, R;
     float beta2, eps;      // Adam only, else 0
+    float dropout;         // edl_set_dropout's rate, else 0
+    uint32_t reserved;
 };
-static_assert(sizeof(SnapshotHeader) == 104, "snapshot header layout");
+static_assert(sizeof(SnapshotHeader) == 112, "snapshot header layout");
 
 // The kernels' scratch (partial results that live inside one pass), in one contiguous piece [scratch_lo, scratch_hi).
 struct Scratch {
@@ -436,6 +439,7 @@ struct edl_handle {
     std::vector<char> bias_waiting;      // ... of them, those whose bias gradient goes with it (2: from the pool after the layer)
     std::vector<char> dw_in_pieces;      // ... those whose weight gradient is there in pieces that are yet to be added up
     bool has_bn = false;
+    float dropout = 0.f;                 // rate at the hidden fully connected layers (edl_set_dropout)
     std::vector<char> op_done;           // a pass: layers already launched out of list order (on the branch stream)
     // backward pass, per tensor: where the gradient "already there" is to be read from if not from the tensor's
     // own gradient buffer (an identity shortcut's part is the masked gradient of the block's output itself)
@@ -895,12 +899,38 @@ int32_t edl_shard(const edl_handle* h, int64_t B, int32_t p, int64_t epoch, int6
     return edl_shard_host(h->seed, h->cfg.N, B, p, epoch, step_in_epoch, out_idx, out_off);
 }
 
+// Whether layer i is a hidden fully connected one: what edl_set_dropout is about.
+static bool hidden_layer(const Graph& g, size_t i) {
+    const Op& op = g.ops[i];
+    if (op.kind != OP_CONV || !op.relu || !op.bias || op.R != 1 || op.S != 1) return false;
+    const Tensor& x = g.tensors[(size_t)op.x];
+    return x.H == 1 && x.W == 1;
+}
+
+// The dropout of layer i in the pass that holds the mini-batch's samples from `first` on, over its activation or the gradient
+// of that: the masks go by the sample's place in the mini-batch, not by the worker, so that they do not depend on p.
+static void drop_out(edl_handle* h, size_t i, void* tensor, int n, int64_t first) {
+    const int C = h->g.ops[i].K;
+    launch_dropout(h->cfg.dtype, tensor, C, tensor, C, n, C, h->dropout, dropout_key(h->seed, h->prog.step, (int)i), (uint64_t)first, h->st);
+}
+
+int32_t edl_set_dropout(edl_handle* h, float rate) {
+    if (!h) { set_error("null handle"); return EDL_EINVAL; }
+    if (!(rate >= 0.f && rate < 1.f)) { set_error("the rate must lie in [0, 1)"); return EDL_EINVAL; }
+    bool any = false;
+    for (size_t i = 0; i < h->g.ops.size(); ++i) any = any || hidden_layer(h->g, i);
+    if (rate > 0.f && !any) { set_error("this model has no hidden fully connected layer"); return EDL_EINVAL; }
+    h->dropout = rate;
+    return EDL_OK;
+}
+
 // Whether the last layer, op i, the loss and their backward pass go in one launch: few outputs over a ReLU layer with a bias that
 // nothing else reads.
 static bool classifier_together(const edl_handle* h, size_t i, const ShardSet& S, const void* weights) {
     const Graph& g = h->g;
     const Op& op = g.ops[i];
     if (i == 0 || op.kind != OP_CONV || op.relu || !op.bias || g.ops[i + 1].kind != OP_LOSS || g.ops[i + 1].x != op.y) return false;
+    if (h->dropout > 0.f && hidden_layer(g, i - 1)) return false;      // (its launch knows no 1 / (1 - rate))
     const Op& prod = g.ops[i - 1];
     const int sx = storage_of(g, op.x);
     return prod.kind == OP_CONV && prod.relu && prod.bias && storage_of(g, prod.y) == sx && sx != 0 && h->readers[(size_t)sx] == 1 &&
@@ -921,8 +951,10 @@ static bool gathers_itself(const edl_handle* h, const ShardSet& S) {
 // single layers from the debugging hooks, which then skip the gather)
 // host_idx: the samples' numbers where the first layer gathers them itself (gathers_itself), else null.
 // train: a backward pass over the same shards follows.  Returns whether the last layer's part of it is done (thin_head_takes).
+// drop_from: where in the mini-batch the pass's samples start, for dropout; -1: there is none (debugging hooks).
 static bool forward_pass(edl_handle* h, const ShardSet& S, const int64_t* dev_idx, float* dev_losses, bool update_running,
-                         size_t op_lo = 0, size_t op_hi = (size_t)-1, const int64_t* host_idx = nullptr, bool train = false) {
+                         size_t op_lo = 0, size_t op_hi = (size_t)-1, const int64_t* host_idx = nullptr, bool train = false,
+                         int64_t drop_from = -1) {
     const int n = S.samples();
     const Graph& g = h->g;
     bool head = false;
@@ -945,6 +977,7 @@ static bool forward_pass(edl_handle* h, const ShardSet& S, const int64_t* dev_id
     float* const partial_held = h->sc<float>(h->L.partial_held);
     RowCut held_sums;
     int held_tensor = -1;
+    auto dropped = [&](size_t i) { return drop_from >= 0 && h->dropout > 0.f && hidden_layer(g, i); };
     auto weights_of = [&](size_t i) {
         const Op& o = g.ops[i];
         const void* wsrc = bf ? (const void*)(h->at<uint16_t>(h->L.shadow) + o.w_off) : (const void*)(h->w() + o.w_off);
@@ -997,6 +1030,7 @@ static bool forward_pass(edl_handle* h, const ShardSet& S, const int64_t* dev_id
                     const SmallInput in = {h->data_x, h->data_y, host_idx, (float*)h->act(0), h->at<int32_t>(h->L.labels)};
                     launch_small_fc_fwd(geom_stored(g, op, n, h->L.in), S, (const float*)h->act(op.x), (const float*)wsrc, op.bias ? h->w() + op.b_off : nullptr,
                                         op.relu, (float*)h->act(op.y), &in, st);
+                    if (dropped(i)) drop_out(h, i, h->act(op.y), n, drop_from);
                     break;
                 }
                 // The classifier, the loss and what their backward pass leaves: the next op is done then
@@ -1033,6 +1067,7 @@ static bool forward_pass(edl_handle* h, const ShardSet& S, const int64_t* dev_id
                 } else {
                     sums = left;
                 }
+                if (dropped(i)) drop_out(h, i, h->act(op.y), n, drop_from);
                 break;
             }
             case OP_BN: {
@@ -1093,9 +1128,11 @@ static double weight_gradient_us(int dt, const ConvGeom& q, int shards) {
 // head: the forward pass has done the last layer's part (forward_pass).
 // held (debugging hook only): tensors whose gradient buffers already hold a contribution the pass adds to.
 // hook: gradients that the pass needs no more are left in their buffers as well (a debugging hook hands them out).
+// drop_from: as in forward_pass.
 static void backward_pass(edl_handle* h, const ShardSet& S, size_t op_lo = 0, size_t op_hi = (size_t)-1, int early_p = 0,
-                          const std::vector<int>* held = nullptr, bool head = false, bool hook = false) {
+                          const std::vector<int>* held = nullptr, bool head = false, bool hook = false, int64_t drop_from = -1) {
     const int n = S.samples();
+    auto dropped = [&](size_t i) { return drop_from >= 0 && h->dropout > 0.f && hidden_layer(h->g, i); };
     // the workers' gradients of the parameters from offset `off` of the flat vector on
     auto grads_at = [&](int64_t off) { return GradDst{h->grad_buf(0) + off, h->L.grad_stride}; };
     const GradDst no_grads = {nullptr, 0};
@@ -1141,7 +1178,8 @@ static void backward_pass(edl_handle* h, const ShardSet& S, size_t op_lo = 0, si
                                  (h->readers[(size_t)sx] == 1 ? !acc : (fuse_joins && acc));
         if (ii > op_lo && last_writer) {
             const Op& prod = g.ops[ii - 1];
-            if (prod.relu && storage_of(g, prod.y) == sx && (prod.kind == OP_BN || prod.kind == OP_CONV)) {
+            // (a dropped layer's gradient is scaled first)
+            if (prod.relu && storage_of(g, prod.y) == sx && (prod.kind == OP_BN || prod.kind == OP_CONV) && !dropped(ii - 1)) {
                 mask.act = h->act(op.x);
                 if (prod.kind == OP_BN) mask.sign = h->sign(op.x);
                 mask.sums = SumsBuf{sums, (size_t)h->L.partial_floats};
@@ -1265,6 +1303,7 @@ static void backward_pass(edl_handle* h, const ShardSet& S, size_t op_lo = 0, si
                     fused_sums.stored = true;
                     break;
                 }
+                if (dropped(ii)) drop_out(h, ii, h->grad(op.y), n, drop_from);
                 const ConvGeom q = geom_stored(g, op, n, h->L.in);
                 // The weight gradient needs only dy (final from here on) and the layer's input, and nothing
                 // before the update reads it: it runs on the second stream, beside the chain of input
@@ -1629,8 +1668,8 @@ static int gradient_passes(edl_handle* h, int32_t p, const int64_t* idx, const i
                 part.off[part.p + 1] = part.off[part.p] + n;
                 part.p += 1;
             }
-            const bool head = forward_pass(h, part, dev_idx + at, dev_losses, first && !alone, 0, (size_t)-1, in_arguments ? stage : nullptr, true);
-            backward_pass(h, part, 0, (size_t)-1, k > last_k && s == S.p ? h->early_p : 0, nullptr, head);
+            const bool head = forward_pass(h, part, dev_idx + at, dev_losses, first && !alone, 0, (size_t)-1, in_arguments ? stage : nullptr, true, at);
+            backward_pass(h, part, 0, (size_t)-1, k > last_k && s == S.p ? h->early_p : 0, nullptr, head, false, at);
             first = false;
             at += part.samples();
         }
@@ -1850,6 +1889,7 @@ int32_t edl_snapshot(edl_handle* h, void* dev_dst, size_t cap, size_t* out_writt
     sh.lr = h->cfg.lr; sh.momentum = h->cfg.momentum; sh.wd = h->cfg.wd; sh.P = P; sh.R = R;
     sh.optimizer = (uint32_t)h->cfg.optimizer;
     if (h->adam()) { sh.beta2 = h->cfg.beta2; sh.eps = h->cfg.eps; }
+    sh.dropout = h->dropout;
     memcpy(&hdr, &sh, sizeof(sh));
     ImageParts parts = state_parts(h);
     float* at = (float*)((char*)dev_dst + EDL_SNAPSHOT_HEADER_BYTES);
@@ -1881,6 +1921,7 @@ int32_t edl_restore(edl_handle* h, const void* dev_src, size_t len) {
         set_error("snapshot header holds Adam coefficients outside their range");
         return EDL_EINVAL;
     }
+    if (!(sh.dropout >= 0.f && sh.dropout < 1.f)) { set_error("snapshot header holds a dropout rate outside [0, 1)"); return EDL_EINVAL; }
     ImageParts parts = state_parts(h);
     const float* at = (const float*)((const char*)dev_src + EDL_SNAPSHOT_HEADER_BYTES);
     for (int q = 0; q < kImageParts; ++q) { parts.dst[q] = (float*)parts.src[q]; parts.src[q] = at; at += parts.n[q]; }
@@ -1891,6 +1932,7 @@ int32_t edl_restore(edl_handle* h, const void* dev_src, size_t len) {
     h->seed = sh.seed;
     h->cfg.lr = sh.lr; h->cfg.momentum = sh.momentum; h->cfg.wd = sh.wd;
     if (h->adam()) { h->cfg.beta2 = sh.beta2; h->cfg.eps = sh.eps; }
+    h->dropout = sh.dropout;
     h->grads_pending = false;               // gradients of the model that was replaced are void
     h->prog.step = sh.step; h->prog.epoch = sh.epoch; h->prog.step_in_epoch = sh.step_in_epoch;
     h->perm_epoch = -1;

@@ -583,7 +583,7 @@ static void build_vgg16(const edl_config& c, Graph& g) {
 // Five biased convolutions with ReLU (11x11/4 pad 2, 5x5 pad 2, three 3x3
 // pad 1; base x {1,3,6,4,4} channels), a 3x3/2 max pool after the first, the
 // second and the fifth, three fully connected layers.  The single-tower form
-// without response normalisation; no dropout.
+// without response normalisation (dropout: edl_set_dropout).
 static void build_alexnet(const edl_config& c, Graph& g) {
     const int H = pick(c.H, 224), W = pick(c.W, 224), C = pick(c.C, 3), classes = pick(c.classes, 1000);
     const int base = pick(c.arch[0], 64), fc = pick(c.arch[1], 4096);

@@ -1,0 +1,264 @@
+"""The operators of a classifier's head on an MI355X against plain references in 64 bits.  Run with -m gpu."""
+import numpy as np
+import pytest
+import torch
+
+import head_reference as R
+
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def E():
+    assert torch.cuda.is_available(), "these tests need the GPU"
+    import paper_1909_11985_amd as E
+    return E
+
+
+def rows_of(gen, rows, cols, pad, dtype, size=1.0, offset=0):
+    """A [rows][cols] view on the GPU whose rows lie cols + pad apart and start `offset` elements into their buffer, and the
+    buffer: what lies between the rows must stay as it is."""
+    buf = (torch.randn(offset + rows * (cols + pad), generator=gen) * size).to(DT[dtype]).cuda()
+    return buf[offset:].view(rows, cols + pad)[:, :cols] if rows else buf[:0].view(0, cols), buf
+
+
+def same_bits(a, b):
+    kind = torch.int32 if a.dtype == torch.float32 else torch.int16
+    return torch.equal(a.contiguous().view(kind).cpu(), b.contiguous().view(kind).cpu())
+
+
+# ---------------------------------------------------------------- dropout
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols,pad,offset,rate,first", [
+    (1, 1, 0, 0, 0.5, 0), (3, 2, 0, 0, 0.5, 7), (1, 7, 0, 0, 0.25, 0), (5, 8, 0, 0, 0.1, 0), (64, 9, 3, 1, 0.9, 1 << 40),
+    (1000, 1, 2, 3, 0.5, 5), (37, 255, 1, 0, 0.3, 0), (300, 24, 0, 0, 0.5, 0), (33, 2047, 0, 1, 0.5, 2 ** 62), (32, 4096, 0, 0, 0.5, 0),
+    (7, 8193, 5, 1, 0.2, 11), (700, 2048, 0, 0, 0.75, 3), (2100, 1000, 24, 0, 0.5, 9), (600, 4097, 1, 1, 0.1, 0), (140000, 16, 0, 0, 0.5, 0)])
+def test_dropout_is_its_definition_to_the_bit(E, dtype, rows, cols, pad, offset, rate, first):
+    """Small calls (one piece per lane) and large ones (four), rows shorter and longer than a block, unaligned ones; the same
+    into a padded result and in place."""
+    gen = torch.Generator().manual_seed(rows * 131 + cols)
+    x, buf = rows_of(gen, rows, cols, pad, dtype, offset=offset)
+    key = R.draw(99, rows + cols)
+    want = R.dropout(x.cpu(), rate, key, first)
+    assert same_bits(E.edl_dropout(x, rate, key, first_row=first), want)
+    out, obuf = rows_of(gen, rows, cols, 5, dtype, offset=1)
+    before = obuf.clone()
+    assert E.edl_dropout(x, rate, key, first_row=first, out=out) is out
+    assert same_bits(out, want)
+    out.copy_(before[1:].view(rows, cols + 5)[:, :cols])
+    assert same_bits(obuf, before)                  # nothing beside the rows was touched
+    before = buf.clone()
+    E.edl_dropout(x, rate, key, first_row=first, out=x)
+    assert same_bits(x, want)
+    x.copy_(before[offset:].view(rows, cols + pad)[:, :cols])
+    assert same_bits(buf, before)
+
+
+def test_dropout_keeps_its_share_and_rate_zero_everything(E):
+    x = torch.ones(512, 4096, device="cuda")
+    for rate in (0.1, 0.5, 0.9):
+        n = int((E.edl_dropout(x, rate, E.edl_dropout_key(3, 4, 5)) != 0).sum())
+        want, spread = x.numel() * (1 - rate), (x.numel() * rate * (1 - rate)) ** 0.5
+        assert abs(n - want) < 6 * spread, (rate, n)
+    y = torch.randn(3, 5, device="cuda")
+    assert same_bits(E.edl_dropout(y, 0.0, 1), y)
+
+
+def test_dropout_drops_what_is_not_finite(E):
+    """A dropped element is +0 whatever it held; a kept one stays what it is."""
+    x = torch.full((64, 64), float("nan"), device="cuda")
+    x[::2] = float("inf")
+    x[1::4] = -1e30
+    y = E.edl_dropout(x, 0.5, 12345).cpu()
+    assert same_bits(y, R.dropout(x.cpu(), 0.5, 12345))
+    assert not torch.isnan(y[torch.from_numpy(~R.kept(64, 64, 0.5, 12345))]).any()
+
+
+def test_dropout_of_rows_in_parts_has_the_masks_of_the_whole(E):
+    x = torch.randn(100, 333, device="cuda")
+    whole = E.edl_dropout(x, 0.5, 77, first_row=10)
+    parts = [E.edl_dropout(x[a:b], 0.5, 77, first_row=10 + a) for a, b in ((0, 1), (1, 40), (40, 100))]
+    assert same_bits(torch.cat(parts), whole)
+
+
+def test_dropout_on_another_stream_and_in_a_replayed_graph(E):
+    x = torch.randn(257, 1025, device="cuda")
+    want = R.dropout(x.cpu(), 0.5, 5)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    y = E.edl_dropout(x, 0.5, 5, stream=side.cuda_stream)
+    side.synchronize()
+    assert same_bits(y, want)
+    with torch.cuda.stream(side):
+        E.edl_dropout(x, 0.5, 5)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        y = E.edl_dropout(x, 0.5, 5)
+    for i in range(3):
+        x.mul_(-2.0)
+        y.zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert same_bits(y, R.dropout(x.cpu(), 0.5, 5)), i
+
+
+def test_dropout_of_nothing(E):
+    for shape in ((0, 5), (5, 0), (0, 0)):
+        assert E.edl_dropout(torch.empty(*shape, device="cuda"), 0.5, 1).shape == shape
+
+
+# ---------------------------------------------------------------- dropout inside a job
+def _net(model, arch, x, params, table, masks, rate, stored):
+    """Logits of MLP, VGG and AlexNet jobs in float64 on the CPU; masks: which elements the hidden layers keep.  Activations
+    are what the job's type stores (a ReLU's sign is taken from those); their rounding passes gradients through."""
+    import torch.nn.functional as F
+    r = lambda t: t + (t.detach().to(stored).double() - t.detach())        # noqa: E731
+    at = {name: (off, size) for name, off, size, _ in table}
+    take = lambda name: params[at[name][0]:at[name][0] + at[name][1]]      # noqa: E731
+
+    def conv(t, name, k, size, stride, pad):
+        w = take(name + ".w").view(k, size, size, t.shape[1]).permute(0, 3, 1, 2)
+        return r(F.relu(F.conv2d(t, w, take(name + ".b"), stride=stride, padding=pad)))
+
+    if model == "vgg16":
+        t, i = x.permute(0, 3, 1, 2), 0
+        for width, times in zip((1, 2, 4, 8, 8), arch[2:7]):
+            for _ in range(times):
+                i += 1
+                t = conv(t, "conv%d" % i, arch[0] * width, 3, 1, 1)
+            t = F.max_pool2d(t, 2, 2)
+        t = t.permute(0, 2, 3, 1)
+    else:
+        t = x
+    t = t.reshape(t.shape[0], -1)
+    for name, mask in zip(("fc1", "fc2"), masks):
+        t = r(F.relu(t @ take(name + ".w").view(-1, t.shape[1]).t() + take(name + ".b")))
+        t = r(torch.where(mask, t / (1.0 - rate), torch.zeros_like(t)))
+    return t @ take("fc3.w").view(-1, t.shape[1]).t() + take("fc3.b")
+
+
+JOBS = {
+    # fully connected nets of vector widths (the small layers' kernels, the classifier's launch) and of odd ones
+    "mlp": dict(model="mlp", geom=dict(H=1, W=1, C_=784, classes=10), arch=(256, 256), N=128, B=64),
+    "mlp_odd": dict(model="mlp", geom=dict(H=1, W=1, C_=37, classes=5), arch=(29, 51), N=48, B=24),
+    "vgg": dict(model="vgg16", geom=dict(H=32, W=32, C_=3, classes=10), arch=(8, 64, 1, 1, 1, 1, 1), N=32, B=16),
+}
+
+
+def _job(E, which, dtype, p_max=4, seed=11, **kw):
+    from paper_1909_11985_amd.binding import make_config
+    import synth_inputs
+    c = JOBS[which]
+    g = c["geom"]
+    x, y = synth_inputs.dataset(2, c["N"], g["H"], g["W"], g["C_"], g["classes"])
+    cfg = make_config(c["model"], dtype=dtype, N=c["N"], B=c["B"], p_max=p_max, lr=0.05, arch=c["arch"], **g, **kw)
+    job = E.Job(cfg, seed)
+    job.bind_dataset(torch.from_numpy(x).cuda(), torch.from_numpy(y).cuda())
+    return job, torch.from_numpy(x).double(), torch.from_numpy(y).long(), E.edl_tensor_table(cfg)
+
+
+def _layers(E, job):
+    """Places of fc1 and fc2 in the layer list: the third and second convolution from its end."""
+    ops = job.debug_op_count()          # ..., fc1, fc2, fc3, loss
+    return ops - 4, ops - 3
+
+
+def _reference(E, job, which, x, y, table, idx, rate, step, seed=11):
+    c = JOBS[which]
+    widths = c["arch"][:2] if c["model"] == "mlp" else (c["arch"][1],) * 2
+    masks = [torch.from_numpy(R.kept(len(idx), n, rate, E.edl_dropout_key(seed, step, layer)))
+             for n, layer in zip(widths, _layers(E, job))]
+    w = torch.from_numpy(job.params()).double().requires_grad_()
+    if job.cfg.dtype == 1:
+        wl = w + (w.detach().to(torch.bfloat16).double() - w.detach())     # what the products read; biases stay float32
+        keep = torch.zeros_like(w, dtype=torch.bool)
+        for name, off, size, _ in table:
+            if name.endswith(".b"):
+                keep[off:off + size] = True
+        wl = torch.where(keep, w, wl)
+        xs = x[idx].to(torch.bfloat16).double()
+    else:
+        wl, xs = w, x[idx]
+    logits = _net(c["model"], c["arch"], xs, wl, table, masks, rate, torch.bfloat16 if job.cfg.dtype == 1 else torch.float32)
+    rows = torch.nn.functional.cross_entropy(logits, y[idx], reduction="none")
+    return rows, w
+
+
+@pytest.mark.parametrize("which,dtype,p,rate", [("mlp", "f32", 1, 0.5), ("mlp", "f32", 4, 0.5), ("mlp_odd", "f32", 3, 0.25), ("mlp", "bf16", 2, 0.5),
+                                                ("vgg", "f32", 2, 0.5), ("vgg", "bf16", 4, 0.3)])
+def test_job_dropout_gradients_are_the_definitions(E, which, dtype, p, rate):
+    """Loss and every worker's gradient at two consecutive steps, against float64 with the masks from the host."""
+    job, x, y, table = _job(E, which, dtype)
+    job.set_dropout(rate)
+    tol = 1e-4 if dtype == "f32" else 2e-2      # what layer-by-layer parity of these jobs is held to
+    for step in range(2):
+        idx, off = job.shard(job.cfg.B, p, *job.progress()[1:])
+        loss = job.gradients(p)
+        rows, w = _reference(E, job, which, x, y, table, idx, rate, step)
+        assert abs(loss - float(rows.detach().mean())) <= tol * max(1.0, abs(loss))
+        for k in range(p):
+            (want,) = torch.autograd.grad(rows[off[k]:off[k + 1]].mean(), w, retain_graph=True)
+            got = torch.from_numpy(job.grad(k)).double()
+            assert float((got - want).norm() / want.norm()) <= tol, (step, k)
+        job.apply(p)
+
+
+@pytest.mark.parametrize("which,dtype", [("mlp", "f32"), ("vgg", "bf16")])
+def test_job_dropout_does_not_depend_on_the_cut(E, which, dtype):
+    """One mini-batch as 1, 2 and 4 shards and as an uneven cut (with an empty shard): the same masks, so the same aggregate."""
+    job, *_ = _job(E, which, dtype)
+    job.set_dropout(0.5)
+    B = job.cfg.B
+    idx, _ = job.shard(B, 1, 0, 0)
+    means = []
+    for off in ([0, B], [0, B // 2, B], [0, B // 4, B // 2, 3 * B // 4, B], [0, 3, 3, B]):
+        off = np.array(off, dtype=np.int64)
+        job.gradients(len(off) - 1, idx, off)
+        share = np.diff(off) / B
+        means.append(sum(s * job.grad(k).astype(np.float64) for k, s in enumerate(share) if s > 0))
+    for m in means[1:]:
+        err = np.linalg.norm(m - means[0]) / np.linalg.norm(means[0])
+        assert err <= (1e-5 if dtype == "f32" else 1e-2), err
+
+
+def test_job_dropout_zero_is_the_job_without_it(E):
+    """Rate 0 takes the launches of a job that never heard of dropout, bit for bit; a rate set and taken back as well."""
+    a, *_ = _job(E, "mlp", "f32")
+    b, *_ = _job(E, "mlp", "f32")
+    b.set_dropout(0.5)
+    b.set_dropout(0.0)
+    for p in (1, 4):
+        assert a.step(p) == b.step(p)
+    assert np.array_equal(a.params(), b.params())
+
+
+def test_job_dropout_travels_with_the_state_image(E):
+    """A joiner created without dropout continues exactly as the job it joined; so does the step without an arena's scratch."""
+    a, *_ = _job(E, "mlp", "f32")
+    a.set_dropout(0.5)
+    a.step(2)
+    b, *_ = _job(E, "mlp", "f32", seed=99)
+    b.restore(a.snapshot())
+    c, *_ = _job(E, "mlp", "f32", seed=98)
+    c.restore(a.snapshot())
+    for p in (4, 1, 2):
+        loss = a.step(p)
+        assert loss == b.step(p) and loss == c.step_static_scratch(p)
+    assert np.array_equal(a.params(), b.params()) and np.array_equal(a.params(), c.params())
+
+
+def test_job_dropout_refusals(E):
+    from paper_1909_11985_amd.binding import make_config
+    job, *_ = _job(E, "mlp", "f32")
+    for rate in (-0.1, 1.0, float("nan")):
+        with pytest.raises(E.EdlError) as ei:
+            job.set_dropout(rate)
+        assert ei.value.code == -1
+    res = E.Job(make_config("resnet20", N=16, B=8, p_max=1, H=16, W=16, C_=3, classes=4, arch=(8, 2, 1)), 1)
+    with pytest.raises(E.EdlError):
+        res.set_dropout(0.5)
+    res.set_dropout(0.0)
