@@ -445,10 +445,38 @@ int32_t edl_adam_update(int32_t p, const float* const* dev_grads, const float* s
  * = its finaliser of key + (j+1) * 0x9E3779B97F4A7C15); an element whose 32 bits are below floor(rate * 2^32) is dropped,
  * to +0 whatever it held.  Rows cut differently over calls (by first_row) have the same masks.  Keys of neighbouring
  * values do not give independent masks; edl_dropout_key (host only) makes one from a seed, a step and a layer.
- * EDL_EINVAL: rate outside [0, 1), negative sizes, bad ld or alignment; EDL_ERANGE: rows * ceil(cols/8) over 2^39. */
+ * EDL_EINVAL: rate outside [0, 1), negative sizes, bad ld or alignment; EDL_ERANGE: rows * ceil(cols/8) over 2^33. */
 int32_t edl_dropout_key(uint64_t seed, int64_t step, int32_t layer, uint64_t* out_key);
 int32_t edl_dropout(int32_t dtype, const void* dev_x, int64_t ldx, void* dev_y, int64_t ldy, int64_t rows, int64_t cols, float rate,
                     uint64_t key, int64_t first_row, void* hip_stream);
+
+/* Of every row of logits [rows][classes] the distribution p = softmax(logits):
+ *   lse[rows]           log sum exp(logits) (needed by the gradient)
+ *   entropy[rows]       -sum p log p
+ *   log_prob[rows]      log p of class dev_targets[row]; 0 where that is no class (negative, or classes and more: a row of padding).
+ *                       dev_targets may be NULL (log_prob is then not written and may be NULL too)
+ *   top_class[rows][k], top_log_prob[rows][k]   the k <= 64 most likely classes, best first, equal ones by the lower number
+ * A logit of -inf masks its class: probability 0, nothing added to the entropy, last among the alternatives.  A row with
+ * nothing but masked classes has lse -inf, entropy 0 and log probabilities -inf.  A NaN or +inf makes everything of its row
+ * NaN (the alternatives' numbers stay classes; NaN ranks as -inf).  Sums are float32, whatever dtype is.
+ * dev_work: edl_log_probs_workspace (host only) bytes, 16-byte aligned; may be NULL if that is 0.  It holds nothing between calls;
+ * calls that overlap need one each.
+ * EDL_EINVAL: null, misaligned or overlapping arguments, classes <= 0, k outside [0, min(64, classes)]; EDL_ENOMEM: workspace
+ * too small; EDL_ERANGE: rows over 2^23 or rows * ceil(classes/8) over 2^33. */
+int32_t edl_log_probs_workspace(int64_t rows, int64_t classes, int32_t k, int64_t* out_bytes);
+int32_t edl_log_probs(int32_t dtype, const void* dev_logits, int64_t ld, int64_t rows, int64_t classes, const int32_t* dev_targets, int32_t k,
+                      float* dev_log_prob, float* dev_entropy, float* dev_lse, float* dev_top_log_prob, int32_t* dev_top_class,
+                      void* dev_work, size_t work_bytes, void* hip_stream);
+
+/* Gradient of the logits for gradients g = dev_dlog_prob[rows] of log_prob and h = dev_dentropy[rows] of entropy (either may be
+ * NULL: zeros), from what edl_log_probs left:
+ *   dlogits = g (1[class = target] - p) - h p (log p + entropy)
+ * in dtype, rounded once; dev_dlogits may be dev_logits (with the same ld).  Masked classes get 0, unless one is the target (g).
+ * Rows without a target take g = 0; a row with g = h = 0 gets zeros whatever its logits are.  dev_targets may be NULL if
+ * dev_dlog_prob is, dev_entropy if dev_dentropy is.  Errors as above. */
+int32_t edl_log_probs_backward(int32_t dtype, const void* dev_logits, int64_t ld, int64_t rows, int64_t classes, const int32_t* dev_targets,
+                               const float* dev_lse, const float* dev_entropy, const float* dev_dlog_prob, const float* dev_dentropy,
+                               void* dev_dlogits, int64_t ldd, void* hip_stream);
 
 /* Measurement: with profiling on, every kernel launch of this library (any
  * handle, and the stand-alone calls) is bracketed by a HIP event pair on the

@@ -5,6 +5,7 @@ never replaced by a fallback: if it is missing, build it with
 `python -m paper_1909_11985_amd.build` (needs hipcc); if that is impossible the
 import fails.
 """
+import collections
 import ctypes as C
 import os
 
@@ -125,6 +126,11 @@ _SIGS = {
     "edl_dropout_key": [C.c_uint64, C.c_int64, C.c_int32, C.POINTER(C.c_uint64)],
     "edl_dropout": [C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_float, C.c_uint64,
                     C.c_int64, C.c_void_p],
+    "edl_log_probs_workspace": [C.c_int64, C.c_int64, C.c_int32, _i64p],
+    "edl_log_probs": [C.c_int32, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
+                      C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p],
+    "edl_log_probs_backward": [C.c_int32, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                               C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p],
     "edl_profile": [C.c_int32],
     "edl_profile_report": [C.c_char_p, C.c_size_t, C.POINTER(C.c_size_t)],
 }
@@ -330,6 +336,57 @@ def edl_dropout(x, rate, key, first_row=0, out=None, stream=None):
             out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         py, ldy = _matrix("out", out, x.shape, x)
         _check(lib.edl_dropout(dt, px, ldx, py, ldy, x.shape[0], x.shape[1], rate, key, first_row, st))
+    return out
+
+
+# What edl_log_probs and edl_classifier_log_probs give: float32 vectors (log_prob None without targets), and with `top`
+# alternatives float32 top_log_prob [rows][top] and int32 top_class [rows][top].
+LogProbs = collections.namedtuple("LogProbs", "log_prob entropy lse top_log_prob top_class")
+
+
+def edl_log_probs_workspace(rows, classes, top=0):
+    n = C.c_int64()
+    _check(lib.edl_log_probs_workspace(rows, classes, top, C.byref(n)))
+    return n.value
+
+
+def edl_log_probs(logits, targets=None, top=0, stream=None):
+    """Log probabilities of the target classes (int32 [rows]; a negative one: none), entropy, log-sum-exp and the `top` most
+    likely classes of rows of logits: a LogProbs."""
+    import torch
+    dt = _dtype_of("logits", logits)
+    pz, ld = _matrix("logits", logits)
+    rows, classes = logits.shape
+    pt = _vector("targets", targets, rows, "torch.int32", logits)
+    need = edl_log_probs_workspace(rows, classes, top)
+    with _On(logits, stream) as st:
+        # one allocation for the float32 results, one for the rest of a call
+        f = torch.empty((3 + top, rows), dtype=torch.float32, device=logits.device)
+        best = torch.empty((rows, top), dtype=torch.int32, device=logits.device) if top > 0 else None
+        work = torch.empty(need, dtype=torch.uint8, device=logits.device) if need else None
+        r = LogProbs(f[0] if targets is not None else None, f[1], f[2], f[3:].view(rows, top) if top > 0 else None, best)
+        base = f.data_ptr()
+        _check(lib.edl_log_probs(dt, pz, ld, rows, classes, pt, top, base if pt else None, base + 4 * rows, base + 8 * rows,
+                                 base + 12 * rows if top > 0 else None, best.data_ptr() if top > 0 else None,
+                                 work.data_ptr() if need else None, need, st))
+    return r
+
+
+def edl_log_probs_backward(logits, targets, lse, entropy, dlog_prob=None, dentropy=None, out=None, stream=None):
+    """Gradient of the logits, in their type, for gradients of log_prob and entropy (None: zeros).  out: where it goes (the
+    logits themselves: in place)."""
+    import torch
+    dt = _dtype_of("logits", logits)
+    pz, ld = _matrix("logits", logits)
+    rows, classes = logits.shape
+    vec = [_vector(name, v, rows, kind, logits) for name, v, kind in (
+        ("targets", targets, "torch.int32"), ("lse", lse, "torch.float32"), ("entropy", entropy, "torch.float32"),
+        ("dlog_prob", dlog_prob, "torch.float32"), ("dentropy", dentropy, "torch.float32"))]
+    with _On(logits, stream) as st:
+        if out is None:
+            out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        pd, ldd = _matrix("out", out, logits.shape, logits)
+        _check(lib.edl_log_probs_backward(dt, pz, ld, rows, classes, *vec, pd, ldd, st))
     return out
 
 

@@ -19,7 +19,7 @@ namespace edl {
 namespace {
 
 constexpr uint64_t kGolden = 0x9E3779B97F4A7C15ull;
-constexpr int kLane = 8;           // elements per lane: four draws, 16 bytes of bf16
+static_assert(kPiece == 8, "a lane's piece is four draws");
 constexpr int64_t kSmallItems = 1 << 18;   // calls of fewer lanes' worth take one piece per lane
 
 __device__ __forceinline__ uint64_t finalise(uint64_t z) {
@@ -29,93 +29,55 @@ __device__ __forceinline__ uint64_t finalise(uint64_t z) {
 }
 
 struct DropoutArgs {
-    int64_t ldx, ldy, rows, cols;
-    int64_t per_row;           // lanes' worth of elements per row
+    Pieces m;
+    int64_t ldx, ldy;
     uint64_t key1, pairs;      // key + golden; draws per row
     uint64_t first_row;
     uint32_t threshold;
     float scale;
 };
 
-template <typename T> __device__ __forceinline__ void load_lane(const T* p, float (&v)[kLane]) {
-    constexpr int VEC = Elem<T>::VEC;
-#pragma unroll
-    for (int q = 0; q < kLane / VEC; ++q) {
-        const Vec16<T> t = load_loose(p + q * VEC);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) v[q * VEC + e] = Elem<T>::to_f32(t.e[e]);
-    }
-}
-__device__ __forceinline__ void store_lane(float* p, const float (&v)[kLane]) {
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
-        Vec16<float> t;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) t.e[e] = v[q * 4 + e];
-        store_loose(p + q * 4, t);
-    }
-}
-__device__ __forceinline__ void store_lane(bf16_t* p, const float (&v)[kLane]) {
-    Vec16<bf16_t> t;
-    t.u = make_uint4(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7]));
-    store_loose(p, t);
-}
-
-// A lane has kLane neighbouring elements of a row at a time, a block U times 256 such pieces in a row.  Products stay in
-// float32 and are rounded once, to nearest even.  U = 4 has four loads in flight and divides once for four pieces (the
+// Products stay in float32 and are rounded once, to nearest even.  U = 4 has four loads in flight and divides once for four pieces (the
 // division of the block's first piece by the pieces of a row takes as long as half a piece's draws); small calls take
 // U = 1, which spreads them over four times the compute units.
 template <typename T, int U>
 __global__ __launch_bounds__(256) void dropout_kernel(const T* x, T* y, DropoutArgs a) {
-    const int64_t item0 = (int64_t)blockIdx.x * (256 * U);
-    const int64_t row0 = item0 / a.per_row, at0 = item0 - row0 * a.per_row;
+    int64_t at0;
+    const int64_t row0 = block_first_row<U>(a.m, at0);
     // addresses and draws from the block's first row on, which are the same for all lanes, in 32x32-bit products
     const T* const x0 = x + row0 * a.ldx;
     T* const y0 = y + row0 * a.ldy;
     const uint64_t j0 = (a.first_row + (uint64_t)row0) * a.pairs;
-    const int64_t rows_left = a.rows - row0;
-    uint32_t row[U];           // from row0
-    int64_t col[U];
-    float v[U][kLane];
+    const int64_t rows_left = a.m.rows - row0;
+    Piece q[U];
+    float v[U][kPiece];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        int64_t at = at0 + u * 256 + (int)threadIdx.x;
-        row[u] = 0;
-        if (at >= a.per_row) {
-            if (a.per_row >= 256 * U) {
-                at -= a.per_row;
-                row[u] = 1;
-            } else {               // at < 2 * 256 * U
-                const unsigned q = (unsigned)at / (unsigned)a.per_row;
-                at -= q * (unsigned)a.per_row;
-                row[u] = q;
-            }
-        }
-        col[u] = at * kLane;
-        if (row[u] < rows_left && col[u] + kLane <= a.cols) load_lane(x0 + (uint64_t)row[u] * (uint32_t)a.ldx + col[u], v[u]);
+        q[u] = piece_of<U>(a.m, at0, u);
+        if (q[u].row < rows_left && q[u].col + kPiece <= a.m.cols) load_piece(x0 + (uint64_t)q[u].row * (uint32_t)a.ldx + q[u].col, v[u]);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        if (row[u] >= rows_left) return;
-        const uint64_t j = j0 + (uint64_t)row[u] * (uint32_t)a.pairs + (uint64_t)col[u] / 2;
+        if (q[u].row >= rows_left) return;
+        const uint64_t j = j0 + (uint64_t)q[u].row * (uint32_t)a.pairs + (uint64_t)q[u].col / 2;
         const uint64_t z = a.key1 + j * kGolden;
-        uint32_t bits[kLane];
+        uint32_t bits[kPiece];
 #pragma unroll
-        for (int i = 0; i < kLane / 2; ++i) {
+        for (int i = 0; i < kPiece / 2; ++i) {
             const uint64_t d = finalise(z + (uint64_t)i * kGolden);
             bits[2 * i] = (uint32_t)d;
             bits[2 * i + 1] = (uint32_t)(d >> 32);
         }
-        T* py = y0 + (uint64_t)row[u] * (uint32_t)a.ldy + col[u];
-        if (col[u] + kLane <= a.cols) {
+        T* py = y0 + (uint64_t)q[u].row * (uint32_t)a.ldy + q[u].col;
+        if (q[u].col + kPiece <= a.m.cols) {
 #pragma unroll
-            for (int e = 0; e < kLane; ++e) v[u][e] = bits[e] >= a.threshold ? v[u][e] * a.scale : 0.f;
-            store_lane(py, v[u]);
+            for (int e = 0; e < kPiece; ++e) v[u][e] = bits[e] >= a.threshold ? v[u][e] * a.scale : 0.f;
+            store_piece(py, v[u]);
         } else {
-            const T* px = x0 + (uint64_t)row[u] * (uint32_t)a.ldx + col[u];
-            const int n = (int)(a.cols - col[u]);
+            const T* px = x0 + (uint64_t)q[u].row * (uint32_t)a.ldx + q[u].col;
+            const int n = (int)(a.m.cols - q[u].col);
 #pragma unroll
-            for (int e = 0; e < kLane; ++e)
+            for (int e = 0; e < kPiece; ++e)
                 if (e < n) py[e] = Elem<T>::from_f32(bits[e] >= a.threshold ? Elem<T>::to_f32(px[e]) * a.scale : 0.f);
         }
     }
@@ -129,9 +91,7 @@ void launch_dropout(int dtype, const void* x, int64_t ldx, void* y, int64_t ldy,
     DropoutArgs a;
     a.ldx = ldx;
     a.ldy = ldy;
-    a.rows = rows;
-    a.cols = cols;
-    a.per_row = (cols + kLane - 1) / kLane;
+    a.m = Pieces{rows, cols, (cols + kPiece - 1) / kPiece};
     a.key1 = key + kGolden;
     a.pairs = ((uint64_t)cols + 1) / 2;
     a.first_row = first_row;
@@ -139,7 +99,7 @@ void launch_dropout(int dtype, const void* x, int64_t ldx, void* y, int64_t ldy,
     a.scale = (float)(1.0 / (1.0 - (double)rate));
     const double esz = dtype == 1 ? 2.0 : 4.0;
     ProfScope ps("dropout", 0.0, 2.0 * esz * (double)rows * (double)cols, st);
-    const int64_t items = rows * a.per_row;                    // (below 2^39, as ldx and ldy are below 2^31: checked by the caller)
+    const int64_t items = rows * a.m.per_row;                    // (up to 2^33, as ldx and ldy are below 2^31: checked by the caller)
     const bool small = items < kSmallItems;
     const unsigned grid = (unsigned)((items + (small ? 255 : 1023)) / (small ? 256 : 1024));
 #define EDL_DROPOUT(TT, UU) hipLaunchKernelGGL((dropout_kernel<TT, UU>), dim3(grid), dim3(256), 0, st, (const TT*)x, (TT*)y, a)

@@ -1,0 +1,303 @@
+// Log probabilities of given classes, entropy and the most likely classes of rows of logits, in one pass over them, and the
+// gradient of the logits.
+//
+// With the running sums of softmax_sums.h a lane reads each logit once; lanes, waves and parts of a row are then joined.
+// Bound: HBM.  A logit costs about 10 issue slots of full-rate instructions (conversion, maximum, one exponential at a
+// quarter of the rate, two sums), of the 14 that reading bf16 at 5.5 TB/s leaves.  The best k ride along: a vector is
+// looked at again only if its largest logit reaches the k-th best of what the wave has seen, which happens
+// k (1 + log(n / k)) times in n logits in random order.
+#include <algorithm>
+
+#include "operators.h"
+#include "profiler.h"
+#include "softmax_sums.h"
+#include "unaligned.h"
+
+namespace edl {
+
+namespace {
+
+struct RowArgs {
+    int64_t ld, rows;
+    uint32_t classes;
+    uint32_t part;             // classes of a part of a row (all of them: rows are not cut)
+    int parts, k;
+    const int32_t* targets;    // null: none
+    float *log_prob, *entropy, *lse, *top_value;
+    int32_t* top_class;
+    float* sums;               // parts > 1: [rows][parts][4]: m, s, t
+    TopKey* keys;              // ... [rows][parts][k]
+};
+
+// One wave writes a row's results.  zt: its target's logit, if it has one.
+__device__ __forceinline__ void write_row(const RowArgs& a, int64_t row, const SoftmaxSums& sums, bool has_target, float zt, const TopKey& top) {
+    const int lane = threadIdx.x & 63;
+    const float lse = softmax_lse(sums);
+    if (lane == 0) {
+        a.lse[row] = lse;
+        a.entropy[row] = softmax_entropy(sums);
+        if (a.targets != nullptr) a.log_prob[row] = has_target ? log_prob_of(zt, lse) : 0.f;
+    }
+    if (lane < a.k) {
+        a.top_value[row * a.k + lane] = log_prob_of(top_value(top), lse);
+        a.top_class[row * a.k + lane] = (int32_t)~top.lo;
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ float target_logit(const RowArgs& a, const T* logits, int64_t row, bool& has) {
+    has = false;
+    if (a.targets == nullptr) return 0.f;
+    const int32_t t = a.targets[row];
+    has = t >= 0 && (uint32_t)t < a.classes;
+    return has ? Elem<T>::to_f32(logits[row * a.ld + t]) : 0.f;
+}
+
+// WAVES = 1: a wave has a row of its own (four to a block); 4: a block has a part of a row.
+template <typename T, int WAVES, bool TOP>
+__global__ __launch_bounds__(256) void log_probs_kernel(const T* __restrict__ logits, RowArgs a) {
+    constexpr int VEC = Elem<T>::VEC, U = 4, STRIDE = WAVES * 64 * VEC;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int64_t row;
+    int part = 0;
+    if (WAVES == 1) {
+        row = (int64_t)blockIdx.x * 4 + wave;
+        if (row >= a.rows) return;
+    } else if (a.parts == 1) {
+        row = blockIdx.x;
+    } else {
+        row = blockIdx.x / (unsigned)a.parts;
+        part = (int)(blockIdx.x - (unsigned)row * (unsigned)a.parts);
+    }
+    const uint32_t lo = (uint32_t)part * a.part, hi = min(lo + a.part, a.classes);
+    const T* const z = logits + row * a.ld;
+    SoftmaxSums sums;
+    TopList top;
+    if (TOP) top.clear();
+    const uint32_t mine = (WAVES == 1 ? lane : threadIdx.x) * VEC;
+    for (uint32_t at = lo; at < hi; at += U * STRIDE) {
+        float v[U][VEC];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t c = at + u * STRIDE + mine;
+            if (c + VEC <= hi) {
+                const Vec16<T> w = load_loose(z + c);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) v[u][e] = Elem<T>::to_f32(w.e[e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) v[u][e] = c + e < hi ? Elem<T>::to_f32(z[c + e]) : -INFINITY;
+            }
+        }
+        float mv[U], m = sums.m;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            mv[u] = v[u][0];
+#pragma unroll
+            for (int e = 1; e < VEC; ++e) mv[u] = fmaxf(mv[u], v[u][e]);
+            m = fmaxf(m, mv[u]);
+        }
+        if (m > sums.m) softmax_rebase(sums, m);
+        const float base = softmax_base(sums);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) softmax_add(sums, v[u][e], base);
+        }
+        if (TOP) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint32_t c = at + u * STRIDE + mine;
+                // (a vector of NaN compares as neither: looked at)
+                if (__ballot(c < hi && !(mv[u] < top.bar)) == 0) continue;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) top.offer(c + e < hi ? top_key(v[u][e], c + e) : TopKey{0, 0}, a.k);
+            }
+        }
+    }
+    softmax_join_wave(sums);
+    if (WAVES == 4) {
+        __shared__ float4 wave_sums[4];
+        __shared__ TopKey wave_keys[TOP ? 4 * 64 : 1];
+        if (lane == 0) wave_sums[wave] = make_float4(sums.m, sums.s, sums.t, 0.f);
+        if (TOP && lane < a.k) wave_keys[wave * a.k + lane] = top.mine;
+        __syncthreads();
+        if (wave != 0) return;
+#pragma unroll
+        for (int w = 1; w < 4; ++w) {
+            SoftmaxSums other;
+            other.m = wave_sums[w].x; other.s = wave_sums[w].y; other.t = wave_sums[w].z;
+            softmax_join(sums, other);
+        }
+        if (TOP)
+            for (int i = a.k; i < 4 * a.k; i += 64) top.offer(i + lane < 4 * a.k ? wave_keys[i + lane] : TopKey{0, 0}, a.k);
+    }
+    if (WAVES == 4 && a.parts > 1) {
+        const int64_t at = row * a.parts + part;
+        if (lane == 0) *reinterpret_cast<float4*>(a.sums + 4 * at) = make_float4(sums.m, sums.s, sums.t, 0.f);
+        if (TOP && lane < a.k) a.keys[at * a.k + lane] = top.mine;
+        return;
+    }
+    bool has;
+    const float zt = target_logit(a, logits, row, has);
+    write_row(a, row, sums, has, zt, top.mine);
+}
+
+// The parts of a row: a wave per row.
+template <typename T, bool TOP>
+__global__ __launch_bounds__(256) void log_probs_join_kernel(const T* __restrict__ logits, RowArgs a) {
+    const int lane = threadIdx.x & 63;
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= a.rows) return;
+    SoftmaxSums sums;
+    if (lane < a.parts) {          // (64 parts at most)
+        const float4 p = *reinterpret_cast<const float4*>(a.sums + 4 * (row * a.parts + lane));
+        sums.m = p.x; sums.s = p.y; sums.t = p.z;
+    }
+    softmax_join_wave(sums);
+    TopList top;
+    if (TOP) {
+        top.clear();
+        const int n = a.parts * a.k;
+        for (int i = 0; i < n; i += 64) top.offer(i + lane < n ? a.keys[row * n + i + lane] : TopKey{0, 0}, a.k);
+    }
+    bool has;
+    const float zt = target_logit(a, logits, row, has);
+    write_row(a, row, sums, has, zt, top.mine);
+}
+
+struct GradArgs {
+    Pieces m;
+    int64_t ld, ldd;
+    const int32_t* targets;
+    const float *lse, *entropy, *dlog_prob, *dentropy;
+};
+
+// dz = g (1[c = t] - p) - h p (log p + H): element-wise once the row's numbers are known, which its lanes read from cache.
+template <typename T, int U>
+__global__ __launch_bounds__(256) void log_probs_grad_kernel(const T* logits, T* dlogits, GradArgs a) {
+    int64_t at0;
+    const int64_t row0 = block_first_row<U>(a.m, at0);
+    const T* const z0 = logits + row0 * a.ld;
+    T* const d0 = dlogits + row0 * a.ldd;
+    const int64_t rows_left = a.m.rows - row0;
+    Piece q[U];
+    float v[U][kPiece];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        q[u] = piece_of<U>(a.m, at0, u);
+        if (q[u].row < rows_left && q[u].col + kPiece <= a.m.cols) load_piece(z0 + (uint64_t)q[u].row * (uint32_t)a.ld + q[u].col, v[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (q[u].row >= rows_left) return;
+        const int64_t row = row0 + q[u].row;
+        const int32_t t = a.targets != nullptr ? a.targets[row] : -1;
+        const bool has = t >= 0 && t < a.m.cols;
+        const float g = has && a.dlog_prob != nullptr ? a.dlog_prob[row] : 0.f;
+        const float h = a.dentropy != nullptr ? a.dentropy[row] : 0.f;
+        const float lse = a.lse[row], both = -(g + (h != 0.f ? h * a.entropy[row] : 0.f));
+        const bool none = g == 0.f && h == 0.f;     // zeros, whatever the logits are
+        const int64_t hot = has ? (int64_t)t - q[u].col : -1;
+        auto grad = [&](float z, int e) {
+            const float lp = z - lse, p = exp_below(lp);
+            const float d = z == -INFINITY ? 0.f : p * (both - h * fmaxf(lp, kFarBelow));
+            return none ? 0.f : e == hot ? d + g : d;
+        };
+        T* pd = d0 + (uint64_t)q[u].row * (uint32_t)a.ldd + q[u].col;
+        if (q[u].col + kPiece <= a.m.cols) {
+#pragma unroll
+            for (int e = 0; e < kPiece; ++e) v[u][e] = grad(v[u][e], e);
+            store_piece(pd, v[u]);
+        } else {
+            const T* pz = z0 + (uint64_t)q[u].row * (uint32_t)a.ld + q[u].col;
+            const int n = (int)(a.m.cols - q[u].col);
+#pragma unroll
+            for (int e = 0; e < kPiece; ++e)
+                if (e < n) pd[e] = Elem<T>::from_f32(grad(Elem<T>::to_f32(pz[e]), e));
+        }
+    }
+}
+
+constexpr int64_t kSmallGradItems = 1 << 18;     // (as in k_dropout.hip)
+constexpr int64_t kWaveClasses = 1024;           // rows up to this length are a wave's
+constexpr int64_t kPartClasses = 4096, kMaxParts = 64, kWantBlocks = 1024;
+
+}  // namespace
+
+// Rows are cut where there are too few to fill the chip: into parts of 4,096 classes at least, towards 1,024 blocks.
+LogProbsPlan plan_log_probs(int64_t rows, int64_t classes, int k) {
+    LogProbsPlan p;
+    p.parts = 1;
+    p.part = classes;
+    if (classes > kWaveClasses && rows > 0) {
+        const int64_t most = std::min<int64_t>(kMaxParts, (classes + kPartClasses - 1) / kPartClasses);
+        const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(most, kWantBlocks / rows));
+        p.part = ((classes + parts - 1) / parts + 7) / 8 * 8;
+        p.parts = (int)((classes + p.part - 1) / p.part);
+    }
+    p.sums_bytes = p.parts > 1 ? (size_t)rows * p.parts * 16 : 0;
+    p.bytes = p.sums_bytes + (p.parts > 1 ? (size_t)rows * p.parts * k * sizeof(TopKey) : 0);
+    return p;
+}
+
+void launch_log_probs(int dtype, const void* logits, int64_t ld, int64_t rows, int64_t classes, const int32_t* targets, int k,
+                      const LogProbsOut& out, void* work, hipStream_t st) {
+    if (rows <= 0) return;
+    const LogProbsPlan p = plan_log_probs(rows, classes, k);
+    RowArgs a = {};
+    a.ld = ld;
+    a.rows = rows;
+    a.classes = (uint32_t)classes;
+    a.part = (uint32_t)p.part;
+    a.parts = p.parts;
+    a.k = k;
+    a.targets = targets;
+    a.log_prob = out.log_prob; a.entropy = out.entropy; a.lse = out.lse; a.top_value = out.top_value; a.top_class = out.top_class;
+    a.sums = (float*)work;
+    a.keys = (TopKey*)((char*)work + p.sums_bytes);
+    const double esz = dtype == 1 ? 2.0 : 4.0;
+    {
+        ProfScope ps("log_probs", 0.0, esz * (double)rows * (double)classes, st);
+        const bool by_wave = classes <= kWaveClasses;
+        const unsigned grid = by_wave ? (unsigned)((rows + 3) / 4) : (unsigned)(rows * p.parts);
+#define EDL_LOG_PROBS(TT, WW, KK) hipLaunchKernelGGL((log_probs_kernel<TT, WW, KK>), dim3(grid), dim3(256), 0, st, (const TT*)logits, a)
+        if (dtype == 1) {
+            if (by_wave) { if (k > 0) EDL_LOG_PROBS(bf16_t, 1, true); else EDL_LOG_PROBS(bf16_t, 1, false); }
+            else { if (k > 0) EDL_LOG_PROBS(bf16_t, 4, true); else EDL_LOG_PROBS(bf16_t, 4, false); }
+        } else {
+            if (by_wave) { if (k > 0) EDL_LOG_PROBS(float, 1, true); else EDL_LOG_PROBS(float, 1, false); }
+            else { if (k > 0) EDL_LOG_PROBS(float, 4, true); else EDL_LOG_PROBS(float, 4, false); }
+        }
+#undef EDL_LOG_PROBS
+    }
+    if (p.parts == 1) return;
+    ProfScope ps("log_probs_join", 0.0, (double)p.bytes, st);
+    const dim3 grid((unsigned)((rows + 3) / 4));
+#define EDL_LOG_PROBS_JOIN(TT, KK) hipLaunchKernelGGL((log_probs_join_kernel<TT, KK>), grid, dim3(256), 0, st, (const TT*)logits, a)
+    if (dtype == 1) { if (k > 0) EDL_LOG_PROBS_JOIN(bf16_t, true); else EDL_LOG_PROBS_JOIN(bf16_t, false); }
+    else { if (k > 0) EDL_LOG_PROBS_JOIN(float, true); else EDL_LOG_PROBS_JOIN(float, false); }
+#undef EDL_LOG_PROBS_JOIN
+}
+
+void launch_log_probs_grad(int dtype, const void* logits, int64_t ld, int64_t rows, int64_t classes, const int32_t* targets, const float* lse,
+                           const float* entropy, const float* dlog_prob, const float* dentropy, void* dlogits, int64_t ldd, hipStream_t st) {
+    if (rows <= 0) return;
+    GradArgs a = {};
+    a.m = Pieces{rows, classes, (classes + kPiece - 1) / kPiece};
+    a.ld = ld;
+    a.ldd = ldd;
+    a.targets = targets;
+    a.lse = lse; a.entropy = entropy; a.dlog_prob = dlog_prob; a.dentropy = dentropy;
+    const double esz = dtype == 1 ? 2.0 : 4.0;
+    ProfScope ps("log_probs_grad", 0.0, 2.0 * esz * (double)rows * (double)classes, st);
+    const int64_t items = rows * a.m.per_row;
+    const bool small = items < kSmallGradItems;
+    const unsigned grid = (unsigned)((items + (small ? 255 : 1023)) / (small ? 256 : 1024));
+#define EDL_LOG_PROBS_GRAD(TT, UU) hipLaunchKernelGGL((log_probs_grad_kernel<TT, UU>), dim3(grid), dim3(256), 0, st, (const TT*)logits, (TT*)dlogits, a)
+    if (dtype == 1) { if (small) EDL_LOG_PROBS_GRAD(bf16_t, 1); else EDL_LOG_PROBS_GRAD(bf16_t, 4); }
+    else { if (small) EDL_LOG_PROBS_GRAD(float, 1); else EDL_LOG_PROBS_GRAD(float, 4); }
+#undef EDL_LOG_PROBS_GRAD
+}
+
+}  // namespace edl

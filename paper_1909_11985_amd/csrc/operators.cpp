@@ -2,7 +2,7 @@
 // See include/edl.h for the contract of every call.
 #include <hip/hip_runtime.h>
 
-#include <cmath>
+#include <initializer_list>
 
 #include "graph.h"
 #include "operators.h"
@@ -10,6 +10,10 @@
 using namespace edl;
 
 namespace {
+
+// A launch has fewer than 2^32 work items: element-wise ones have one for up to four pieces of eight elements, others a
+// block of 256 for a row.
+constexpr int64_t kMaxPieces = 1ll << 33, kMaxRows = 1ll << 23;
 
 int launched() {
     const hipError_t e = hipGetLastError();
@@ -54,8 +58,64 @@ int32_t edl_dropout(int32_t dtype, const void* dev_x, int64_t ldx, void* dev_y, 
     if (rows == 0 || cols == 0) return EDL_OK;
     if (!rows_ok("x", dtype, dev_x, rows, cols, ldx) || !rows_ok("y", dtype, dev_y, rows, cols, ldy)) return EDL_EINVAL;
     if (dev_x == dev_y && rows > 1 && ldx != ldy) { set_error("in place, x and y need the same ld"); return EDL_EINVAL; }
-    if (cols > INT32_MAX || rows > (1ll << 39) / ((cols + 7) / 8)) { set_error("%lld x %lld elements are too many", (long long)rows, (long long)cols); return EDL_ERANGE; }
+    if (cols > INT32_MAX || rows > kMaxPieces / ((cols + 7) / 8)) { set_error("%lld x %lld elements are too many", (long long)rows, (long long)cols); return EDL_ERANGE; }
     launch_dropout(dtype, dev_x, ldx, dev_y, ldy, rows, cols, rate, key, (uint64_t)first_row, (hipStream_t)hip_stream);
+    return launched();
+}
+
+// what the calls over rows of logits have in common; EDL_OK if there is something to do
+static int32_t check_logits(int32_t dtype, int64_t rows, int64_t classes) {
+    if (!known_dtype(dtype)) return EDL_EINVAL;
+    if (rows < 0 || classes <= 0) { set_error("rows must not be negative, classes positive"); return EDL_EINVAL; }
+    if (classes > INT32_MAX || rows > kMaxRows || rows * ((classes + 7) / 8) > kMaxPieces) { set_error("%lld x %lld logits are too many", (long long)rows, (long long)classes); return EDL_ERANGE; }
+    return EDL_OK;
+}
+
+static bool vectors_aligned(std::initializer_list<const void*> v) {
+    for (const void* p : v)
+        if ((uintptr_t)p % 4) { set_error("a vector is not aligned to its elements"); return false; }
+    return true;
+}
+
+int32_t edl_log_probs_workspace(int64_t rows, int64_t classes, int32_t k, int64_t* out_bytes) {
+    if (!out_bytes) { set_error("null argument"); return EDL_EINVAL; }
+    const int32_t rc = check_logits(EDL_DTYPE_F32, rows, classes);
+    if (rc) return rc;
+    if (k < 0 || k > kMaxTop || k > classes) { set_error("k=%d outside [0, min(%d, classes)]", k, kMaxTop); return EDL_EINVAL; }
+    *out_bytes = (int64_t)plan_log_probs(rows, classes, k).bytes;
+    return EDL_OK;
+}
+
+int32_t edl_log_probs(int32_t dtype, const void* dev_logits, int64_t ld, int64_t rows, int64_t classes, const int32_t* dev_targets, int32_t k,
+                      float* dev_log_prob, float* dev_entropy, float* dev_lse, float* dev_top_log_prob, int32_t* dev_top_class,
+                      void* dev_work, size_t work_bytes, void* hip_stream) {
+    const int32_t rc = check_logits(dtype, rows, classes);
+    if (rc) return rc;
+    if (k < 0 || k > kMaxTop || k > classes) { set_error("k=%d outside [0, min(%d, classes)]", k, kMaxTop); return EDL_EINVAL; }
+    if (rows == 0) return EDL_OK;
+    if (!rows_ok("logits", dtype, dev_logits, rows, classes, ld)) return EDL_EINVAL;
+    if (!dev_entropy || !dev_lse || (dev_targets && !dev_log_prob) || (k > 0 && (!dev_top_log_prob || !dev_top_class))) { set_error("null argument"); return EDL_EINVAL; }
+    if (!vectors_aligned({dev_targets, dev_log_prob, dev_entropy, dev_lse, dev_top_log_prob, dev_top_class})) return EDL_EINVAL;
+    const LogProbsPlan p = plan_log_probs(rows, classes, k);
+    if (work_bytes < p.bytes) { set_error("workspace of %zu bytes is smaller than the %zu needed", work_bytes, p.bytes); return EDL_ENOMEM; }
+    if (p.bytes > 0 && (!dev_work || (uintptr_t)dev_work % 16)) { set_error("the workspace must be 16-byte aligned"); return EDL_EINVAL; }
+    launch_log_probs(dtype, dev_logits, ld, rows, classes, dev_targets, k, LogProbsOut{dev_log_prob, dev_entropy, dev_lse, dev_top_log_prob, dev_top_class},
+                     dev_work, (hipStream_t)hip_stream);
+    return launched();
+}
+
+int32_t edl_log_probs_backward(int32_t dtype, const void* dev_logits, int64_t ld, int64_t rows, int64_t classes, const int32_t* dev_targets,
+                               const float* dev_lse, const float* dev_entropy, const float* dev_dlog_prob, const float* dev_dentropy,
+                               void* dev_dlogits, int64_t ldd, void* hip_stream) {
+    const int32_t rc = check_logits(dtype, rows, classes);
+    if (rc) return rc;
+    if (rows == 0) return EDL_OK;
+    if (!rows_ok("logits", dtype, dev_logits, rows, classes, ld) || !rows_ok("dlogits", dtype, dev_dlogits, rows, classes, ldd)) return EDL_EINVAL;
+    if (dev_logits == dev_dlogits && rows > 1 && ld != ldd) { set_error("in place, logits and dlogits need the same ld"); return EDL_EINVAL; }
+    if (!dev_lse || (dev_dentropy && !dev_entropy) || (dev_dlog_prob && !dev_targets)) { set_error("null argument"); return EDL_EINVAL; }
+    if (!vectors_aligned({dev_targets, dev_lse, dev_entropy, dev_dlog_prob, dev_dentropy})) return EDL_EINVAL;
+    launch_log_probs_grad(dtype, dev_logits, ld, rows, classes, dev_targets, dev_lse, dev_entropy, dev_dlog_prob, dev_dentropy, dev_dlogits, ldd,
+                          (hipStream_t)hip_stream);
     return launched();
 }
 

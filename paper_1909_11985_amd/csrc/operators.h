@@ -16,4 +16,14 @@ void launch_dropout(int dtype, const void* x, int64_t ldx, void* y, int64_t ldy,
 // The key of one layer's masks in one step of a job.
 uint64_t dropout_key(uint64_t seed, int64_t step, int layer);
 
+// ---- log probabilities --------------------------------------------------------
+constexpr int kMaxTop = 64;        // one lane of a wave each
+struct LogProbsPlan { int parts; int64_t part; size_t sums_bytes, bytes; };      // parts of a row; bytes of workspace
+LogProbsPlan plan_log_probs(int64_t rows, int64_t classes, int k);
+struct LogProbsOut { float *log_prob, *entropy, *lse, *top_value; int32_t* top_class; };
+void launch_log_probs(int dtype, const void* logits, int64_t ld, int64_t rows, int64_t classes, const int32_t* targets, int k,
+                      const LogProbsOut& out, void* work, hipStream_t st);
+void launch_log_probs_grad(int dtype, const void* logits, int64_t ld, int64_t rows, int64_t classes, const int32_t* targets, const float* lse,
+                           const float* entropy, const float* dlog_prob, const float* dentropy, void* dlogits, int64_t ldd, hipStream_t st);
+
 }  // namespace edl

@@ -37,3 +37,42 @@ def dropout(x, rate, key, first_row=0):
     scale = np.float32(1.0 / (1.0 - float(np.float32(rate))))
     y = x.float() * torch.tensor(scale)
     return torch.where(torch.from_numpy(kept(*x.shape, rate, key, first_row)), y, torch.zeros_like(y)).to(x.dtype)
+
+
+def log_probs(z, targets, top=0):
+    """(log_prob, entropy, lse, top_log_prob, top_class) of rows of float64 logits, as include/edl.h defines them."""
+    rows, classes = z.shape
+    bad = (torch.isnan(z) | (z == math.inf)).any(1)
+    empty = (z == -math.inf).all(1)
+    safe = torch.where((bad | empty)[:, None], torch.zeros_like(z), z)
+    lse = torch.logsumexp(safe, 1)
+    lp = safe - lse[:, None]
+    p = lp.exp()
+    entropy = -torch.where(p > 0, p * lp, torch.zeros_like(p)).sum(1)
+    nan, inf = torch.full_like(lse, math.nan), torch.full_like(lse, -math.inf)
+    lse = torch.where(bad, nan, torch.where(empty, inf, lse))
+    entropy = torch.where(bad, nan, torch.where(empty, torch.zeros_like(entropy), entropy))
+    lp = torch.where(bad[:, None], nan[:, None], torch.where(empty[:, None], inf[:, None], lp))
+    log_prob = None
+    if targets is not None:
+        has = (targets >= 0) & (targets < classes)
+        at = torch.where(has, targets, torch.zeros_like(targets)).long()
+        log_prob = torch.where(has, lp.gather(1, at[:, None])[:, 0], torch.zeros_like(lse))
+    rank = torch.where(torch.isnan(z), torch.full_like(z, -math.inf), z)
+    order = torch.sort(rank, dim=1, descending=True, stable=True).indices[:, :top]
+    return log_prob, entropy, lse, lp.gather(1, order), order.to(torch.int32)
+
+
+def log_probs_backward(z, targets, dlog_prob, dentropy):
+    """Gradient of rows of float64 logits, from the formula."""
+    rows, classes = z.shape
+    _, entropy, lse, _, _ = log_probs(z, None)
+    has = torch.zeros(rows, dtype=torch.bool) if targets is None else (targets >= 0) & (targets < classes)
+    g = torch.where(has, dlog_prob.double() if dlog_prob is not None else torch.zeros(rows, dtype=torch.float64), torch.zeros(rows, dtype=torch.float64))
+    h = dentropy.double() if dentropy is not None else torch.zeros(rows, dtype=torch.float64)
+    lp = z - lse[:, None]
+    p = torch.where(z == -math.inf, torch.zeros_like(z), lp.exp())
+    d = -g[:, None] * p - h[:, None] * torch.where(p > 0, p * (lp + entropy[:, None]), p)
+    for r in torch.nonzero(has)[:, 0].tolist():
+        d[r, int(targets[r])] += g[r]
+    return torch.where(((g == 0) & (h == 0))[:, None], torch.zeros_like(d), d)

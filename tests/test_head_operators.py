@@ -111,6 +111,214 @@ def test_dropout_of_nothing(E):
         assert E.edl_dropout(torch.empty(*shape, device="cuda"), 0.5, 1).shape == shape
 
 
+# ---------------------------------------------------------------- log probabilities
+# Float32 sums of n terms each: an absolute error of the logit's rounding, 2^-24 (|z| + |lse|) for the difference z - lse, and
+# of the sum's relative error.  Terms are joined over lanes of at most ~n / 64 / parts sequential additions of 2^-24 each, plus
+# the exponential's 2 ulp and its argument's 2^-24 |z - m|: (n / 64 + 2 + |z - m|) 2^-24, n <= 200,000 -> 2e-4 worst case of
+# all errors aligned; they are not, their signs alternate, and the root of n / 64 stands for n / 64.
+def stat_tolerance(z, classes):
+    finite = torch.where(torch.isfinite(z), z.abs(), torch.zeros_like(z))
+    return 2.0 ** -24 * (4 + (classes / 64) ** 0.5 + 4 * float(finite.max()))
+
+
+def logits_of(gen, rows, classes, pad, dtype, size=3.0, masked=0.0, offset=0):
+    z, buf = rows_of(gen, rows, classes, pad, dtype, size, offset)
+    if masked:
+        z[torch.rand(rows, classes, generator=gen).cuda() < masked] = -float("inf")
+    return z, buf
+
+
+def targets_of(gen, rows, classes):
+    t = torch.randint(0, classes, (rows,), generator=gen, dtype=torch.int32)
+    t[torch.rand(rows, generator=gen) < 0.2] = -1
+    return t
+
+
+def check_stats(r, want, tol, top):
+    log_prob, entropy, lse, top_lp, top_cls = want
+    for got, ref in ((r.log_prob, log_prob), (r.entropy, entropy), (r.lse, lse)) + (((r.top_log_prob, top_lp),) if top else ()):
+        if got is None:
+            assert ref is None
+            continue
+        got = got.cpu().double()
+        fine = torch.isfinite(ref)
+        assert torch.equal(torch.isnan(got), torch.isnan(ref)) and torch.equal(got[got.isinf()], ref[ref.isinf()])
+        assert torch.equal(torch.isfinite(got), fine)
+        if fine.any():
+            assert float((got - ref)[fine].abs().max()) <= tol
+    if top:
+        assert torch.equal(r.top_class.cpu(), top_cls)
+
+
+SHAPES = [(1, 1, 0, 0, 1, 0), (1, 2, 0, 0, 2, 0), (5, 3, 0, 0, 1, 1), (9, 10, 0, 0, 0, 0), (256, 1000, 0, 0, 5, 0), (3, 1023, 1, 1, 64, 0.3), (6, 1024, 0, 0, 3, 0),
+          (6, 1025, 0, 1, 3, 0.9), (2, 4097, 3, 1, 20, 0), (1, 32000, 0, 0, 5, 0), (3, 50001, 5, 1, 40, 0.3), (700, 2051, 0, 0, 7, 0), (65, 8200, 8, 0, 64, 0),
+          (1, 200003, 0, 1, 64, 0), (1030, 1500, 0, 0, 0, 0.5), (4, 4096, 0, 0, 10, 0), (2, 262150, 0, 0, 1, 0)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,classes,pad,offset,top,masked", SHAPES)
+def test_log_probs(E, dtype, rows, classes, pad, offset, top, masked):
+    """A wave per row, a block per row, rows in parts; odd lengths, unaligned rows, masked classes, rows without a target."""
+    gen = torch.Generator().manual_seed(rows * 7 + classes)
+    z, _ = logits_of(gen, rows, classes, pad, dtype, masked=min(masked, 0.95), offset=offset)
+    t = targets_of(gen, rows, classes)
+    zc = z.cpu().double()
+    r = E.edl_log_probs(z, t.cuda(), top=top)
+    check_stats(r, R.log_probs(zc, t, top), stat_tolerance(zc, classes), top)
+    again = E.edl_log_probs(z, t.cuda(), top=top)
+    for a, b in zip(r, again):
+        assert a is None or torch.equal(a.view(torch.int32), b.view(torch.int32))
+    if top < 2:
+        q = E.edl_log_probs(z, None, top=top)
+        assert q.log_prob is None and torch.equal(q.lse, r.lse) and torch.equal(q.entropy, r.entropy)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,classes", [(8, 100), (8, 3000), (8, 20000)])
+def test_log_probs_of_rows_at_their_edges(E, dtype, rows, classes):
+    """One class left; all masked; all equal (ties by the lower number); the type's lowest value as a mask; NaN; +inf; large
+    values that differ little; signed zeros."""
+    gen = torch.Generator().manual_seed(classes)
+    z = (torch.randn(rows, classes, generator=gen) * 2).to(DT[dtype])
+    lowest = torch.finfo(DT[dtype]).min
+    z[0] = -float("inf")
+    z[0, classes // 2] = 1.5
+    z[1] = -float("inf")
+    z[2] = 0.25
+    z[3, : classes - 3] = lowest
+    z[4, classes - 1] = float("nan")
+    z[5, 3] = float("inf")
+    z[6] = 1000.0
+    z[7] = -0.0
+    z[7, 1::2] = 0.0
+    t = torch.tensor([classes // 2, 0, classes - 1, 2, 0, 3, -5, classes], dtype=torch.int32)
+    top = 20
+    r = E.edl_log_probs(z.cuda(), t.cuda(), top=top)
+    zc = z.double()
+    fine = torch.where(zc <= lowest, torch.full_like(zc, -1e30), zc)      # the lowest value's log probability is itself: checked apart
+    want = R.log_probs(torch.where(zc == -float("inf"), zc, fine), t, top)
+    got = E.LogProbs(r.log_prob.clone(), r.entropy, r.lse, r.top_log_prob.clone(), r.top_class)
+    assert float(r.log_prob[3]) == float(lowest) and bool((r.top_log_prob[3, 3:] == lowest).all())
+    want[0][3] = 0.0
+    want[3][3, 3:] = 0.0
+    got.log_prob[3] = 0.0
+    got.top_log_prob[3, 3:] = 0.0
+    check_stats(got, want, 2.0 ** -24 * (4 + classes ** 0.5 / 8 + 4 * 1000.0), top)
+
+
+def test_log_probs_in_rising_order_and_of_equal_logits(E):
+    """Every class beats all before it (the list of the best changes with each), and falling and equal ones."""
+    for dtype in (torch.float32, torch.bfloat16):
+        up = torch.arange(9000, dtype=torch.float32).mul(0.001).to(dtype)
+        z = torch.stack([up, up.flip(0), torch.zeros_like(up), up.abs().sub(4).abs()])
+        r = E.edl_log_probs(z.cuda(), None, top=64)
+        zc = z.double()
+        check_stats(r, R.log_probs(zc, None, 64), stat_tolerance(zc, 9000), 64)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,classes,pad,offset,top,masked", SHAPES)
+def test_log_probs_backward(E, dtype, rows, classes, pad, offset, top, masked):
+    """Against the formula; padded, in place, and with either gradient missing.  Tolerance: half a step of the result, and the
+    float32 error of p (that of z - lse) times the gradients."""
+    gen = torch.Generator().manual_seed(rows * 11 + classes)
+    z, buf = logits_of(gen, rows, classes, pad, dtype, masked=min(masked, 0.95), offset=offset)
+    t = targets_of(gen, rows, classes)
+    r = E.edl_log_probs(z, t.cuda())
+    g, h = torch.randn(rows, generator=gen), torch.randn(rows, generator=gen) * 0.3
+    g[rows // 2] = 0.0
+    h[rows // 2] = 0.0
+    zc = z.cpu().double()
+    alive = torch.isfinite(R.log_probs(zc, None)[2])
+    for dg, dh in ((g, h), (g, None), (None, h)):
+        want = R.log_probs_backward(zc, t, dg, dh)
+        want = torch.where(alive[:, None] | (want == 0), want, torch.nan_to_num(want))
+        d = E.edl_log_probs_backward(z, t.cuda(), r.lse, r.entropy, None if dg is None else dg.cuda(), None if dh is None else dh.cuda())
+        got = d.cpu().double()
+        size = (0 if dg is None else g.abs()) + (0 if dh is None else h.abs() * 15)     # p (log p + H): H and -p log p stay below 13
+        tol = R.EPS[DT[dtype]] * want.abs() + (size[:, None] * stat_tolerance(zc, classes))
+        assert bool(((got - want).abs() <= tol)[alive].all())
+        assert bool((got[rows // 2] == 0).all())
+    before = buf.clone()
+    assert E.edl_log_probs_backward(z, t.cuda(), r.lse, r.entropy, None, h.cuda(), out=z) is z
+    assert same_bits(z, d)
+    z.copy_(before[offset:].view(rows, classes + pad)[:, :classes])
+    assert same_bits(buf, before)
+
+
+def test_log_probs_backward_against_differences(E):
+    """Central differences of the loss g log_prob + h entropy in float64 at a few classes of every row."""
+    gen = torch.Generator().manual_seed(3)
+    z = (torch.randn(6, 40, generator=gen) * 2)
+    t = torch.tensor([0, 39, -1, 7, 8, 20], dtype=torch.int32)
+    g, h = torch.randn(6, generator=gen), torch.randn(6, generator=gen)
+    r = E.edl_log_probs(z.cuda(), t.cuda())
+    d = E.edl_log_probs_backward(z.cuda(), t.cuda(), r.lse, r.entropy, g.cuda(), h.cuda()).cpu().double()
+
+    def loss(zz):
+        lp, H, *_ = R.log_probs(zz, t)
+        return g.double() * lp + h.double() * H
+    step = 1e-5
+    for c in (0, 7, 8, 20, 39, 11):
+        e = torch.zeros(6, 40, dtype=torch.float64)
+        e[:, c] = step
+        diff = (loss(z.double() + e) - loss(z.double() - e)) / (2 * step)
+        # the difference quotient's error: step^2 times third derivatives (of size |g| + 6 |h|), and 2^-52 x 20 / step
+        assert float((diff - d[:, c]).abs().max()) <= 1e-6
+
+
+def test_log_probs_backward_of_rows_without_a_distribution(E):
+    """All masked: zeros (and the target's g).  NaN rows: NaN, unless nothing is wanted of them."""
+    z = torch.full((4, 1500), -float("inf"))
+    z[2:] = float("nan")
+    t = torch.tensor([-1, 5, -1, -1], dtype=torch.int32)
+    r = E.edl_log_probs(z.cuda(), t.cuda())
+    h = torch.tensor([1.0, 1.0, 0.0, 1.0])
+    d = E.edl_log_probs_backward(z.cuda(), t.cuda(), r.lse, r.entropy, torch.full((4,), 2.0).cuda(), h.cuda()).cpu()
+    assert bool((d[0] == 0).all()) and float(d[1, 5]) == 2.0 and float(d[1].abs().sum()) == 2.0
+    assert bool((d[2] == 0).all()) and bool(torch.isnan(d[3]).all())
+
+
+def test_log_probs_in_a_replayed_graph_and_on_another_stream(E):
+    gen = torch.Generator().manual_seed(5)
+    z = (torch.randn(4, 20000, generator=gen) * 3).cuda()
+    t = torch.tensor([1, 2, -1, 19999], dtype=torch.int32).cuda()
+    g = torch.randn(4, generator=gen).cuda()
+
+    def call(stream=None):
+        r = E.edl_log_probs(z, t, top=9, stream=stream)
+        return (*r, E.edl_log_probs_backward(z, t, r.lse, r.entropy, g, g, stream=stream))
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    on_side = call(side.cuda_stream)
+    side.synchronize()
+    eager = call()
+    for a, b in zip(on_side, eager):
+        assert torch.equal(a, b)
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = call()
+    for i in range(3):
+        z.add_(torch.randn(4, 20000, generator=gen).cuda())
+        want = call()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(held, want):
+            assert torch.equal(a, b), i
+
+
+def test_log_probs_of_no_rows(E):
+    z = torch.empty(0, 7, device="cuda")
+    t = torch.empty(0, dtype=torch.int32, device="cuda")
+    r = E.edl_log_probs(z, t, top=3)
+    assert r.lse.shape == (0,) and r.top_class.shape == (0, 3)
+    assert E.edl_log_probs_backward(z, t, r.lse, r.entropy, r.lse, r.lse).shape == (0, 7)
+
+
 # ---------------------------------------------------------------- dropout inside a job
 def _net(model, arch, x, params, table, masks, rate, stored):
     """Logits of MLP, VGG and AlexNet jobs in float64 on the CPU; masks: which elements the hidden layers keep.  Activations

@@ -46,7 +46,7 @@ def test_reference_masks_agree_with_the_scalar_generator():
     (dict(dtype=2), -1), (dict(x=None), -1), (dict(y=None), -1), (dict(rows=-1), -1), (dict(cols=-1), -1), (dict(first=-1), -1),
     (dict(rate=1.0), -1), (dict(rate=-0.01), -1), (dict(rate=float("nan")), -1), (dict(ldx=15), -1), (dict(ldy=15), -1),
     (dict(ldx=2 ** 31), -1), (dict(x=SOME + 2), -1), (dict(y=SOME + 1, dtype=1), -1), (dict(y=SOME, ldy=17), -1),
-    (dict(rows=2 ** 38, cols=24, ldx=24, ldy=24), -4)])
+    (dict(rows=2 ** 33, cols=24, ldx=24, ldy=24), -4)])
 def test_dropout_refusals(E, change, code):
     a = dict(dtype=0, x=SOME, ldx=16, y=2 * SOME, ldy=16, rows=4, cols=16, rate=0.5, first=0)
     a.update(change)
@@ -59,3 +59,47 @@ def test_binding_refuses_what_is_no_matrix_on_a_gpu(E):
         with pytest.raises(E.EdlError) as ei:
             E.edl_dropout(x, 0.5, 1)
         assert ei.value.code == -1
+
+
+LOG_PROBS = dict(dtype=0, z=SOME, ld=100, rows=4, classes=100, t=SOME, k=3, lp=SOME, ent=SOME, lse=SOME, tv=SOME, tc=SOME, work=None, bytes=0)
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(dtype=-1), -1), (dict(z=None), -1), (dict(z=SOME + 2), -1), (dict(ld=99), -1), (dict(rows=-1), -1), (dict(classes=0), -1),
+    (dict(k=-1), -1), (dict(k=65), -1), (dict(k=4, classes=3, ld=3), -1), (dict(lp=None), -1), (dict(ent=None), -1), (dict(lse=None), -1),
+    (dict(tv=None), -1), (dict(tc=None), -1), (dict(lse=SOME + 2), -1), (dict(t=SOME + 1), -1), (dict(classes=20000, ld=20000), -3),
+    (dict(classes=20000, ld=20000, work=None, bytes=1 << 20), -1), (dict(classes=20000, ld=20000, work=SOME + 8, bytes=1 << 20), -1),
+    (dict(rows=2 ** 23 + 1), -4), (dict(rows=2 ** 22, classes=2 ** 20, ld=2 ** 20), -4)])
+def test_log_probs_refusals(E, change, code):
+    a = dict(LOG_PROBS)
+    a.update(change)
+    rc = E.lib.edl_log_probs(a["dtype"], a["z"], a["ld"], a["rows"], a["classes"], a["t"], a["k"], a["lp"], a["ent"], a["lse"], a["tv"], a["tc"],
+                             a["work"], a["bytes"], None)
+    assert rc == code and E.lib.edl_last_error()
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(dtype=7), -1), (dict(z=None), -1), (dict(d=None), -1), (dict(ldd=99), -1), (dict(lse=None), -1), (dict(ent=None), -1), (dict(t=None), -1),
+    (dict(d=SOME, ldd=101), -1), (dict(d=SOME + 1, dtype=1), -1), (dict(g=SOME + 2), -1), (dict(classes=-3), -1), (dict(rows=2 ** 30), -4)])
+def test_log_probs_backward_refusals(E, change, code):
+    a = dict(dtype=0, z=SOME, ld=100, rows=4, classes=100, t=SOME, lse=SOME, ent=SOME, g=SOME, h=SOME, d=2 * SOME, ldd=100)
+    a.update(change)
+    rc = E.lib.edl_log_probs_backward(a["dtype"], a["z"], a["ld"], a["rows"], a["classes"], a["t"], a["lse"], a["ent"], a["g"], a["h"], a["d"], a["ldd"], None)
+    assert rc == code and E.lib.edl_last_error()
+
+
+def test_log_probs_workspace(E):
+    assert E.edl_log_probs_workspace(256, 1000, 5) == 0 and E.edl_log_probs_workspace(5000, 100000, 64) == 0 and E.edl_log_probs_workspace(0, 10, 0) == 0
+    assert E.edl_log_probs_workspace(1, 32000, 5) == 8 * (16 + 5 * 8)          # eight parts of 4,000
+    for bad in ((1, 0, 0), (-1, 5, 0), (1, 5, 6), (1, 100, 65)):
+        with pytest.raises(E.EdlError) as ei:
+            E.edl_log_probs_workspace(*bad)
+        assert ei.value.code == -1
+
+
+def test_parts_of_a_row_cover_it(E):
+    """What the plan promises: no part empty, none beyond 64, workspace whole parts."""
+    for rows in (1, 2, 17, 63, 300, 1023, 1024, 5000):
+        for classes in (1, 8, 1024, 1025, 4096, 4097, 8193, 49999, 200000, 262145, 10 ** 7):
+            n = E.edl_log_probs_workspace(rows, classes, 0)
+            assert n % (16 * rows) == 0 and n // (16 * rows) <= 64 and n // (16 * rows) != 1
