@@ -3,9 +3,11 @@
 //
 // With the running sums of softmax_sums.h a lane reads each logit once; lanes, waves and parts of a row are then joined.
 // Bound: HBM.  A logit costs about 10 issue slots of full-rate instructions (conversion, maximum, one exponential at a
-// quarter of the rate, two sums), of the 14 that reading bf16 at 5.5 TB/s leaves.  The best k ride along: a vector is
-// looked at again only if its largest logit reaches the k-th best of what the wave has seen, which happens
-// k (1 + log(n / k)) times in n logits in random order.
+// quarter of the rate, two sums), of the 14 that reading bf16 at 5.5 TB/s leaves.  The best k ride along: after a round of
+// loads only vectors that reach the k-th best of what the wave has seen are put aside in LDS and then entered into the
+// wave's list, k log(rounds) of their logits in random order beside the first round's, whose bound is the k-th of the 64
+// lanes' largest.  Entering them where they lie, in registers, means that code once for each of a lane's 32
+// logits: 11 KB of instructions, whose first fetch alone took most of the 13 us of a call for one row.
 #include <algorithm>
 
 #include "operators.h"
@@ -32,14 +34,13 @@ struct RowArgs {
 // One wave writes a row's results.  zt: its target's logit, if it has one.
 __device__ __forceinline__ void write_row(const RowArgs& a, int64_t row, const SoftmaxSums& sums, bool has_target, float zt, const TopKey& top) {
     const int lane = threadIdx.x & 63;
-    const float lse = softmax_lse(sums);
     if (lane == 0) {
-        a.lse[row] = lse;
+        a.lse[row] = softmax_lse(sums);
         a.entropy[row] = softmax_entropy(sums);
-        if (a.targets != nullptr) a.log_prob[row] = has_target ? log_prob_of(zt, lse) : 0.f;
+        if (a.targets != nullptr) a.log_prob[row] = has_target ? softmax_log_prob(sums, zt) : 0.f;
     }
     if (lane < a.k) {
-        a.top_value[row * a.k + lane] = log_prob_of(top_value(top), lse);
+        a.top_value[row * a.k + lane] = softmax_log_prob(sums, top_value(top));
         a.top_class[row * a.k + lane] = (int32_t)~top.lo;
     }
 }
@@ -56,7 +57,11 @@ __device__ __forceinline__ float target_logit(const RowArgs& a, const T* logits,
 // WAVES = 1: a wave has a row of its own (four to a block); 4: a block has a part of a row.
 template <typename T, int WAVES, bool TOP>
 __global__ __launch_bounds__(256) void log_probs_kernel(const T* __restrict__ logits, RowArgs a) {
-    constexpr int VEC = Elem<T>::VEC, U = 4, STRIDE = WAVES * 64 * VEC;
+    constexpr int VEC = Elem<T>::VEC, U = 4, WIDE = 64 * VEC, STRIDE = WAVES * WIDE;
+    // a wave's vectors of one round that hold candidates, and which of the wave's vectors of the round each is
+    __shared__ uint4 aside[TOP ? 4 : 1][TOP ? U * 64 : 1];
+    __shared__ uint8_t aside_at[TOP ? 4 : 1][TOP ? U * 64 : 1];
+    __shared__ TopKey scratch[TOP ? 4 : 1][TOP ? 64 : 1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int64_t row;
     int part = 0;
@@ -76,43 +81,64 @@ __global__ __launch_bounds__(256) void log_probs_kernel(const T* __restrict__ lo
     if (TOP) top.clear();
     const uint32_t mine = (WAVES == 1 ? lane : threadIdx.x) * VEC;
     for (uint32_t at = lo; at < hi; at += U * STRIDE) {
-        float v[U][VEC];
+        Vec16<T> w[U];
+        if (at + U * STRIDE <= hi) {           // (the same for all lanes: the loads follow each other without a branch)
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const uint32_t c = at + u * STRIDE + mine;
-            if (c + VEC <= hi) {
-                const Vec16<T> w = load_loose(z + c);
+            for (int u = 0; u < U; ++u) w[u] = load_loose(z + at + u * STRIDE + mine);
+        } else {
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) v[u][e] = Elem<T>::to_f32(w.e[e]);
-            } else {
+            for (int u = 0; u < U; ++u) {
+                const uint32_t c = at + u * STRIDE + mine;
+                if (c + VEC <= hi) {
+                    w[u] = load_loose(z + c);
+                } else {
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) v[u][e] = c + e < hi ? Elem<T>::to_f32(z[c + e]) : -INFINITY;
+                    for (int e = 0; e < VEC; ++e) w[u].e[e] = c + e < hi ? z[c + e] : Elem<T>::from_f32(-INFINITY);
+                }
             }
         }
-        float mv[U], m = sums.m;
+        float mv[U], round = -INFINITY;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            mv[u] = v[u][0];
+            mv[u] = Elem<T>::to_f32(w[u].e[0]);
 #pragma unroll
-            for (int e = 1; e < VEC; ++e) mv[u] = fmaxf(mv[u], v[u][e]);
-            m = fmaxf(m, mv[u]);
+            for (int e = 1; e < VEC; ++e) mv[u] = fmaxf(mv[u], Elem<T>::to_f32(w[u].e[e]));
+            round = fmaxf(round, mv[u]);
         }
-        if (m > sums.m) softmax_rebase(sums, m);
+        if (round > sums.m) softmax_rebase(sums, round);
         const float base = softmax_base(sums);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) softmax_add(sums, v[u][e], base);
+            for (int e = 0; e < VEC; ++e) softmax_add(sums, Elem<T>::to_f32(w[u].e[e]), base);
         }
         if (TOP) {
+            if (at == lo) top.expect(at + mine < hi ? top_key(round, 0).hi : 0, a.k);
+            const float bar = top.bar();
+            if (__ballot(at + mine < hi && !(round < bar)) == 0) continue;
+            int n = 0;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const uint32_t c = at + u * STRIDE + mine;
-                // (a vector of NaN compares as neither: looked at)
-                if (__ballot(c < hi && !(mv[u] < top.bar)) == 0) continue;
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) top.offer(c + e < hi ? top_key(v[u][e], c + e) : TopKey{0, 0}, a.k);
+                const bool in = at + u * STRIDE + mine < hi && !(mv[u] < bar);
+                const uint64_t who = __ballot(in);
+                if (in) {
+                    const int to = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+                    aside[wave][to] = w[u].u;
+                    aside_at[wave][to] = (uint8_t)(u * 64 + lane);
+                }
+                n += __popcll(who);
             }
+            wave_lds_handover();
+            for (int i = lane; i - lane < n * VEC; i += 64) {
+                TopKey c = {0, 0};
+                if (i < n * VEC) {
+                    const int p = aside_at[wave][i / VEC];
+                    const uint32_t cls = at + (p >> 6) * STRIDE + (WAVES == 1 ? 0 : wave * WIDE) + (p & 63) * VEC + i % VEC;
+                    if (cls < hi) c = top_key(Elem<T>::to_f32(reinterpret_cast<const T*>(aside[wave])[i]), cls);
+                }
+                top.offer(c, a.k, scratch[wave]);
+            }
+            wave_lds_handover();
         }
     }
     softmax_join_wave(sums);
@@ -129,8 +155,14 @@ __global__ __launch_bounds__(256) void log_probs_kernel(const T* __restrict__ lo
             other.m = wave_sums[w].x; other.s = wave_sums[w].y; other.t = wave_sums[w].z;
             softmax_join(sums, other);
         }
-        if (TOP)
-            for (int i = a.k; i < 4 * a.k; i += 64) top.offer(i + lane < 4 * a.k ? wave_keys[i + lane] : TopKey{0, 0}, a.k);
+        if (TOP) {
+            // a wave's k-th has k - 1 before it: what is worse than the best of those is none of the block's best
+            for (int w = 1; w < 4; ++w) {
+                const TopKey t = wave_keys[w * a.k + a.k - 1];
+                if (t.hi != 0) top.raise(TopKey{t.hi, t.lo - 1});
+            }
+            for (int i = a.k; i < 4 * a.k; i += 64) top.offer(i + lane < 4 * a.k ? wave_keys[i + lane] : TopKey{0, 0}, a.k, scratch[0]);
+        }
     }
     if (WAVES == 4 && a.parts > 1) {
         const int64_t at = row * a.parts + part;
@@ -146,6 +178,7 @@ __global__ __launch_bounds__(256) void log_probs_kernel(const T* __restrict__ lo
 // The parts of a row: a wave per row.
 template <typename T, bool TOP>
 __global__ __launch_bounds__(256) void log_probs_join_kernel(const T* __restrict__ logits, RowArgs a) {
+    __shared__ TopKey scratch[TOP ? 4 : 1][TOP ? 64 : 1];
     const int lane = threadIdx.x & 63;
     const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     if (row >= a.rows) return;
@@ -159,7 +192,10 @@ __global__ __launch_bounds__(256) void log_probs_join_kernel(const T* __restrict
     if (TOP) {
         top.clear();
         const int n = a.parts * a.k;
-        for (int i = 0; i < n; i += 64) top.offer(i + lane < n ? a.keys[row * n + i + lane] : TopKey{0, 0}, a.k);
+        uint32_t best = 0;
+        for (int i = lane; i < n; i += 64) best = max(best, a.keys[row * n + i].hi);
+        top.expect(best, a.k);
+        for (int i = 0; i < n; i += 64) top.offer(i + lane < n ? a.keys[row * n + i + lane] : TopKey{0, 0}, a.k, scratch[threadIdx.x >> 6]);
     }
     bool has;
     const float zt = target_logit(a, logits, row, has);
@@ -200,7 +236,7 @@ __global__ __launch_bounds__(256) void log_probs_grad_kernel(const T* logits, T*
         const bool none = g == 0.f && h == 0.f;     // zeros, whatever the logits are
         const int64_t hot = has ? (int64_t)t - q[u].col : -1;
         auto grad = [&](float z, int e) {
-            const float lp = z - lse, p = exp_below(lp);
+            const float lp = z - lse, p = exp2_of(lp * kLog2e);
             const float d = z == -INFINITY ? 0.f : p * (both - h * fmaxf(lp, kFarBelow));
             return none ? 0.f : e == hot ? d + g : d;
         };

@@ -206,6 +206,22 @@ def test_log_probs_of_rows_at_their_edges(E, dtype, rows, classes):
     check_stats(got, want, 2.0 ** -24 * (4 + classes ** 0.5 / 8 + 4 * 1000.0), top)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_log_probs_of_the_types_largest_values(E, dtype):
+    """Rows of nothing but the lowest value (every class masked alike: all equally likely), of the largest, and of both."""
+    big = torch.finfo(DT[dtype]).max
+    for classes in (70, 1500, 9001):
+        z = torch.full((3, classes), -big, dtype=DT[dtype])
+        z[1] = big
+        z[2, 5] = big
+        r = E.edl_log_probs(z.cuda(), torch.tensor([3, 4, 5], dtype=torch.int32).cuda(), top=1)
+        assert r.lse.cpu().tolist() == [-big, big, big]          # log(classes) is far below a step
+        H, lp = r.entropy.cpu(), r.log_prob.cpu()
+        assert r.top_class[:, 0].tolist() == [0, 0, 5] and torch.equal(lp, r.top_log_prob[:, 0].cpu())
+        assert abs(float(lp[0]) + np.log(classes)) < 1e-5 and abs(float(lp[1]) + np.log(classes)) < 1e-5 and float(lp[2]) == 0.0
+        assert abs(float(H[0]) - np.log(classes)) < 1e-5 and abs(float(H[1]) - np.log(classes)) < 1e-5 and float(H[2]) == 0.0
+
+
 def test_log_probs_in_rising_order_and_of_equal_logits(E):
     """Every class beats all before it (the list of the best changes with each), and falling and equal ones."""
     for dtype in (torch.float32, torch.bfloat16):
