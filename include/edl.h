@@ -436,7 +436,7 @@ int32_t edl_adam_update(int32_t p, const float* const* dev_grads, const float* s
  * only; nothing between rows is read or written.  Work is queued on hip_stream (NULL: the default stream), which has to
  * belong to the current device, as all pointers have to; nothing is allocated, nothing synchronises, and every call may be
  * captured into a graph.  Results do not depend on anything but the arguments: no atomics, the same bits every time.
- * Calls of no rows return EDL_OK and touch nothing. */
+ * Calls of no rows return EDL_OK and touch nothing, unless it says otherwise. */
 
 /* y = kept ? x / (1 - rate) : 0 for a [rows][cols] matrix, rounded once; y may be x (with the same ld) and must not
  * overlap it otherwise.  No mask is stored: whether element (r, c) is kept follows from (key, first_row + r, c) and cols
@@ -477,6 +477,31 @@ int32_t edl_log_probs(int32_t dtype, const void* dev_logits, int64_t ld, int64_t
 int32_t edl_log_probs_backward(int32_t dtype, const void* dev_logits, int64_t ld, int64_t rows, int64_t classes, const int32_t* dev_targets,
                                const float* dev_lse, const float* dev_entropy, const float* dev_dlog_prob, const float* dev_dentropy,
                                void* dev_dlogits, int64_t ldd, void* hip_stream);
+
+/* edl_log_probs (without alternatives) of the logits x w^T + bias, which are not stored: x [rows][dim] features, w [classes][dim]
+ * weights, both in dtype, bias float32 [classes] or NULL; sums in float32.  A bias of -inf masks its class, targets, results and
+ * rows at their edges are as there; x and w must be finite.
+ * dev_work: edl_classifier_workspace (host only; the pointers are looked at for their alignment only, NULL: any) bytes, 256-byte
+ * aligned, which hold nothing between calls; calls that overlap need one each.  x and w are read where they lie if address, ld and dim are multiples of
+ * 16 bytes (and ld at most 2^23 bytes); else the call copies them into the workspace first, rows padded to whole 16 bytes.
+ * EDL_EINVAL: null, misaligned or overlapping arguments, dim or classes <= 0; EDL_ENOMEM: workspace too small; EDL_ERANGE: rows over 2^23,
+ * dim over 2^16, classes over 2^24, rows * dim over 2^31, classes * dim over 2^34, ceil(rows/128) * ceil(classes/128) over 2^23. */
+int32_t edl_classifier_workspace(int32_t dtype, const void* dev_x, int64_t ldx, const void* dev_w, int64_t ldw, int64_t rows, int64_t dim,
+                                 int64_t classes, int32_t backward, int64_t* out_bytes);
+int32_t edl_classifier_log_probs(int32_t dtype, const void* dev_x, int64_t ldx, const void* dev_w, int64_t ldw, const float* dev_bias, int64_t rows,
+                                 int64_t dim, int64_t classes, const int32_t* dev_targets, float* dev_log_prob, float* dev_entropy, float* dev_lse,
+                                 void* dev_work, size_t work_bytes, void* hip_stream);
+
+/* Gradients for gradients g = dev_dlog_prob[rows] of log_prob and h = dev_dentropy[rows] of entropy (either may be NULL: zeros):
+ * with dz as in edl_log_probs_backward, dx = dz w in dtype, dw = dz^T x and dbias = sum of dz over the rows in float32 (what
+ * edl_average_update and edl_adam_update take; dev_dbias may be NULL).  The logits are formed again, a piece of the classes at a
+ * time, and dz is stored for such a piece (at most 256 MiB of workspace, or 128 classes): in bf16 as a sum of three bf16 numbers, so that dw
+ * and dbias are float32 results.  All outputs are written, not added to; of no rows, dw and dbias are zeros.  Arguments and errors as
+ * above; the workspace's size is another (backward = 1). */
+int32_t edl_classifier_log_probs_backward(int32_t dtype, const void* dev_x, int64_t ldx, const void* dev_w, int64_t ldw, const float* dev_bias,
+                                          int64_t rows, int64_t dim, int64_t classes, const int32_t* dev_targets, const float* dev_lse,
+                                          const float* dev_entropy, const float* dev_dlog_prob, const float* dev_dentropy, void* dev_dx, int64_t lddx,
+                                          float* dev_dw, int64_t lddw, float* dev_dbias, void* dev_work, size_t work_bytes, void* hip_stream);
 
 /* Measurement: with profiling on, every kernel launch of this library (any
  * handle, and the stand-alone calls) is bracketed by a HIP event pair on the

@@ -9,5 +9,6 @@ from .binding import (  # noqa: F401
     edl_query, edl_arena_bytes, edl_shard_host, edl_init_params_host, edl_tensor_table,
     edl_adam_update, edl_average_update, edl_copy, edl_mfma_rate, edl_profile, edl_profile_report, lib,
     edl_dropout, edl_dropout_key, LogProbs, edl_log_probs_workspace, edl_log_probs, edl_log_probs_backward,
+    edl_classifier_workspace, edl_classifier_log_probs, edl_classifier_log_probs_backward,
     edl_set_option, edl_get_option, options,
 )

@@ -131,6 +131,12 @@ _SIGS = {
                       C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p],
     "edl_log_probs_backward": [C.c_int32, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p],
+    "edl_classifier_workspace": [C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_int64, C.c_int32, _i64p],
+    "edl_classifier_log_probs": [C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_int64,
+                                 C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p],
+    "edl_classifier_log_probs_backward": [C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_int64,
+                                          C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p,
+                                          C.c_int64, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p],
     "edl_profile": [C.c_int32],
     "edl_profile_report": [C.c_char_p, C.c_size_t, C.POINTER(C.c_size_t)],
 }
@@ -388,6 +394,74 @@ def edl_log_probs_backward(logits, targets, lse, entropy, dlog_prob=None, dentro
         pd, ldd = _matrix("out", out, logits.shape, logits)
         _check(lib.edl_log_probs_backward(dt, pz, ld, rows, classes, *vec, pd, ldd, st))
     return out
+
+
+def _classifier(x, w, bias, targets):
+    dt = _dtype_of("x", x)
+    px, ldx = _matrix("x", x)
+    rows, dim = x.shape
+    pw, ldw = _matrix("w", w, (w.shape[0], dim) if w.dim() == 2 else None, x)
+    classes = w.shape[0]
+    pb = _vector("bias", bias, classes, "torch.float32", x)
+    pt = _vector("targets", targets, rows, "torch.int32", x)
+    return dt, px, ldx, pw, ldw, pb, rows, dim, classes, pt
+
+
+def edl_classifier_workspace(x, w, backward=False):
+    """Bytes of workspace that edl_classifier_log_probs (or its gradient) of these features and weights takes."""
+    dt, px, ldx, pw, ldw, _, rows, dim, classes, _ = _classifier(x, w, None, None)
+    n = C.c_int64()
+    _check(lib.edl_classifier_workspace(dt, px, ldx, pw, ldw, rows, dim, classes, 1 if backward else 0, C.byref(n)))
+    return n.value
+
+
+def _workspace(need, work, like):
+    import torch
+    if work is None:
+        return torch.empty(need, dtype=torch.uint8, device=like.device) if need else None
+    if str(work.dtype) != "torch.uint8" or work.device != like.device or not work.is_contiguous():
+        _refuse("the workspace must be a contiguous uint8 tensor on %s" % like.device)
+    return work
+
+
+def edl_classifier_log_probs(x, w, bias=None, targets=None, work=None, stream=None):
+    """edl_log_probs (without alternatives) of the logits x w^T + bias, which are not stored.  x: [rows][dim], w: [classes][dim]
+    of the same type, bias: float32 [classes].  work: uint8 workspace (None: a new one)."""
+    import torch
+    args = _classifier(x, w, bias, targets)
+    rows = x.shape[0]
+    with _On(x, stream) as st:
+        work = _workspace(edl_classifier_workspace(x, w) if work is None else 0, work, x)
+        f = torch.empty((3, rows), dtype=torch.float32, device=x.device)
+        base = f.data_ptr()
+        _check(lib.edl_classifier_log_probs(*args, base if targets is not None else None, base + 4 * rows, base + 8 * rows,
+                                            None if work is None else work.data_ptr(), 0 if work is None else work.numel(), st))
+    return LogProbs(f[0] if targets is not None else None, f[1], f[2], None, None)
+
+
+def edl_classifier_log_probs_backward(x, w, bias, targets, lse, entropy, dlog_prob=None, dentropy=None, work=None, stream=None,
+                                      dx=None, dw=None, dbias=None):
+    """(dx, dw, dbias): gradients of the features in their type and of weights and bias in float32 (dbias None without a
+    bias), for gradients of log_prob and entropy (None: zeros).  dx, dw, dbias: where they go (None: new tensors)."""
+    import torch
+    args = _classifier(x, w, bias, targets)
+    rows, dim = x.shape
+    classes = w.shape[0]
+    vec = [_vector(name, v, rows, "torch.float32", x) for name, v in (("lse", lse), ("entropy", entropy), ("dlog_prob", dlog_prob), ("dentropy", dentropy))]
+    with _On(x, stream) as st:
+        work = _workspace(edl_classifier_workspace(x, w, True) if work is None else 0, work, x)
+        dx = torch.empty((rows, dim), dtype=x.dtype, device=x.device) if dx is None else dx
+        dw = torch.empty((classes, dim), dtype=torch.float32, device=x.device) if dw is None else dw
+        if bias is not None and dbias is None:
+            dbias = torch.empty(classes, dtype=torch.float32, device=x.device)
+        pdx, lddx = _matrix("dx", dx, (rows, dim), x)
+        pdw, lddw = _matrix("dw", dw, (classes, dim))
+        if str(dw.dtype) != "torch.float32" or dw.device != x.device:
+            _refuse("dw must be float32 on %s" % x.device)
+        pdb = _vector("dbias", dbias, classes, "torch.float32", x)
+        _check(lib.edl_classifier_log_probs_backward(*args, *vec, pdx, lddx, pdw, lddw, pdb, None if work is None else work.data_ptr(),
+                                                     0 if work is None else work.numel(), st))
+    return dx, dw, dbias
 
 
 def edl_set_option(name, value):

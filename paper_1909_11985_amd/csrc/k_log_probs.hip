@@ -205,11 +205,10 @@ __global__ __launch_bounds__(256) void log_probs_join_kernel(const T* __restrict
 struct GradArgs {
     Pieces m;
     int64_t ld, ldd;
-    const int32_t* targets;
-    const float *lse, *entropy, *dlog_prob, *dentropy;
+    RowFacts facts;
 };
 
-// dz = g (1[c = t] - p) - h p (log p + H): element-wise once the row's numbers are known, which its lanes read from cache.
+// Element-wise once the row's numbers are known, which its lanes read from cache.
 template <typename T, int U>
 __global__ __launch_bounds__(256) void log_probs_grad_kernel(const T* logits, T* dlogits, GradArgs a) {
     int64_t at0;
@@ -227,19 +226,9 @@ __global__ __launch_bounds__(256) void log_probs_grad_kernel(const T* logits, T*
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         if (q[u].row >= rows_left) return;
-        const int64_t row = row0 + q[u].row;
-        const int32_t t = a.targets != nullptr ? a.targets[row] : -1;
-        const bool has = t >= 0 && t < a.m.cols;
-        const float g = has && a.dlog_prob != nullptr ? a.dlog_prob[row] : 0.f;
-        const float h = a.dentropy != nullptr ? a.dentropy[row] : 0.f;
-        const float lse = a.lse[row], both = -(g + (h != 0.f ? h * a.entropy[row] : 0.f));
-        const bool none = g == 0.f && h == 0.f;     // zeros, whatever the logits are
-        const int64_t hot = has ? (int64_t)t - q[u].col : -1;
-        auto grad = [&](float z, int e) {
-            const float lp = z - lse, p = exp2_of(lp * kLog2e);
-            const float d = z == -INFINITY ? 0.f : p * (both - h * fmaxf(lp, kFarBelow));
-            return none ? 0.f : e == hot ? d + g : d;
-        };
+        const LogitGrad row = logit_grad(a.facts, row0 + q[u].row, a.m.cols);
+        const int64_t hot = row.target - q[u].col;
+        auto grad = [&](float z, int e) { return row.of(z, e == hot); };
         T* pd = d0 + (uint64_t)q[u].row * (uint32_t)a.ldd + q[u].col;
         if (q[u].col + kPiece <= a.m.cols) {
 #pragma unroll
@@ -323,8 +312,7 @@ void launch_log_probs_grad(int dtype, const void* logits, int64_t ld, int64_t ro
     a.m = Pieces{rows, classes, (classes + kPiece - 1) / kPiece};
     a.ld = ld;
     a.ldd = ldd;
-    a.targets = targets;
-    a.lse = lse; a.entropy = entropy; a.dlog_prob = dlog_prob; a.dentropy = dentropy;
+    a.facts = RowFacts{targets, lse, entropy, dlog_prob, dentropy};
     const double esz = dtype == 1 ? 2.0 : 4.0;
     ProfScope ps("log_probs_grad", 0.0, 2.0 * esz * (double)rows * (double)classes, st);
     const int64_t items = rows * a.m.per_row;

@@ -13,7 +13,7 @@ namespace {
 
 // A launch has fewer than 2^32 work items: element-wise ones have one for up to four pieces of eight elements, others a
 // block of 256 for a row.
-constexpr int64_t kMaxPieces = 1ll << 33, kMaxRows = 1ll << 23;
+constexpr int64_t kMaxPieces = 1ll << 33, kMaxRows = 1ll << 23, kMaxDim = 1 << 16, kMaxClasses = 1 << 24, kMaxTiles = 1 << 23;
 
 int launched() {
     const hipError_t e = hipGetLastError();
@@ -116,6 +116,74 @@ int32_t edl_log_probs_backward(int32_t dtype, const void* dev_logits, int64_t ld
     if (!vectors_aligned({dev_targets, dev_lse, dev_entropy, dev_dlog_prob, dev_dentropy})) return EDL_EINVAL;
     launch_log_probs_grad(dtype, dev_logits, ld, rows, classes, dev_targets, dev_lse, dev_entropy, dev_dlog_prob, dev_dentropy, dev_dlogits, ldd,
                           (hipStream_t)hip_stream);
+    return launched();
+}
+
+// what the calls over features and classifier weights have in common
+static int32_t check_classifier(int32_t dtype, int64_t rows, int64_t dim, int64_t classes) {
+    if (!known_dtype(dtype)) return EDL_EINVAL;
+    if (rows < 0 || dim <= 0 || classes <= 0) { set_error("rows must not be negative, dim and classes positive"); return EDL_EINVAL; }
+    if (rows > kMaxRows || dim > kMaxDim || classes > kMaxClasses || rows * dim > (1ll << 31) || classes * dim > (1ll << 34) ||
+        ((rows + 127) / 128) * ((classes + 127) / 128) > kMaxTiles) {
+        set_error("%lld rows of %lld features for %lld classes are too many", (long long)rows, (long long)dim, (long long)classes);
+        return EDL_ERANGE;
+    }
+    return EDL_OK;
+}
+
+static int32_t check_work(const ClassifierCall& c, bool backward, size_t work_bytes) {
+    const size_t need = classifier_work_bytes(c, backward);
+    if (work_bytes < need) { set_error("workspace of %zu bytes is smaller than the %zu needed", work_bytes, need); return EDL_ENOMEM; }
+    if (need > 0 && (!c.work || (uintptr_t)c.work % 256)) { set_error("the workspace must be 256-byte aligned"); return EDL_EINVAL; }
+    return EDL_OK;
+}
+
+int32_t edl_classifier_workspace(int32_t dtype, const void* dev_x, int64_t ldx, const void* dev_w, int64_t ldw, int64_t rows, int64_t dim,
+                                 int64_t classes, int32_t backward, int64_t* out_bytes) {
+    if (!out_bytes) { set_error("null argument"); return EDL_EINVAL; }
+    const int32_t rc = check_classifier(dtype, rows, dim, classes);
+    if (rc) return rc;
+    ClassifierCall c = {};
+    c.dtype = dtype; c.x = dev_x; c.ldx = ldx; c.w = dev_w; c.ldw = ldw; c.rows = rows; c.dim = dim; c.classes = classes;
+    *out_bytes = rows == 0 ? 0 : (int64_t)classifier_work_bytes(c, backward != 0);
+    return EDL_OK;
+}
+
+int32_t edl_classifier_log_probs(int32_t dtype, const void* dev_x, int64_t ldx, const void* dev_w, int64_t ldw, const float* dev_bias, int64_t rows,
+                                 int64_t dim, int64_t classes, const int32_t* dev_targets, float* dev_log_prob, float* dev_entropy, float* dev_lse,
+                                 void* dev_work, size_t work_bytes, void* hip_stream) {
+    int32_t rc = check_classifier(dtype, rows, dim, classes);
+    if (rc) return rc;
+    if (rows == 0) return EDL_OK;
+    if (!rows_ok("x", dtype, dev_x, rows, dim, ldx) || !rows_ok("w", dtype, dev_w, classes, dim, ldw)) return EDL_EINVAL;
+    if (!dev_entropy || !dev_lse || (dev_targets && !dev_log_prob)) { set_error("null argument"); return EDL_EINVAL; }
+    if (!vectors_aligned({dev_bias, dev_targets, dev_log_prob, dev_entropy, dev_lse})) return EDL_EINVAL;
+    const ClassifierCall c = {dtype, dev_x, ldx, dev_w, ldw, dev_bias, rows, dim, classes, dev_targets, dev_work};
+    rc = check_work(c, false, work_bytes);
+    if (rc) return rc;
+    launch_classifier(c, ClassifierOut{dev_log_prob, dev_entropy, dev_lse}, (hipStream_t)hip_stream);
+    return launched();
+}
+
+int32_t edl_classifier_log_probs_backward(int32_t dtype, const void* dev_x, int64_t ldx, const void* dev_w, int64_t ldw, const float* dev_bias,
+                                          int64_t rows, int64_t dim, int64_t classes, const int32_t* dev_targets, const float* dev_lse,
+                                          const float* dev_entropy, const float* dev_dlog_prob, const float* dev_dentropy, void* dev_dx, int64_t lddx,
+                                          float* dev_dw, int64_t lddw, float* dev_dbias, void* dev_work, size_t work_bytes, void* hip_stream) {
+    int32_t rc = check_classifier(dtype, rows, dim, classes);
+    if (rc) return rc;
+    if (!rows_ok("dw", EDL_DTYPE_F32, dev_dw, classes, dim, lddw)) return EDL_EINVAL;
+    if (rows > 0) {
+        if (!rows_ok("x", dtype, dev_x, rows, dim, ldx) || !rows_ok("w", dtype, dev_w, classes, dim, ldw) || !rows_ok("dx", dtype, dev_dx, rows, dim, lddx))
+            return EDL_EINVAL;
+        if (!dev_lse || (dev_dentropy && !dev_entropy) || (dev_dlog_prob && !dev_targets)) { set_error("null argument"); return EDL_EINVAL; }
+    }
+    if (!vectors_aligned({dev_bias, dev_targets, dev_lse, dev_entropy, dev_dlog_prob, dev_dentropy, dev_dbias})) return EDL_EINVAL;
+    const ClassifierCall c = {dtype, dev_x, ldx, dev_w, ldw, dev_bias, rows, dim, classes, dev_targets, dev_work};
+    if (rows > 0) {
+        rc = check_work(c, true, work_bytes);
+        if (rc) return rc;
+    }
+    launch_classifier_grads(c, ClassifierGrads{dev_lse, dev_entropy, dev_dlog_prob, dev_dentropy, dev_dx, lddx, dev_dw, lddw, dev_dbias}, (hipStream_t)hip_stream);
     return launched();
 }
 

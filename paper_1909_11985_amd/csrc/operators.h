@@ -26,4 +26,30 @@ void launch_log_probs(int dtype, const void* logits, int64_t ld, int64_t rows, i
 void launch_log_probs_grad(int dtype, const void* logits, int64_t ld, int64_t rows, int64_t classes, const int32_t* targets, const float* lse,
                            const float* entropy, const float* dlog_prob, const float* dentropy, void* dlogits, int64_t ldd, hipStream_t st);
 
+// ---- classifier ------------------------------------------------------------------
+struct ClassifierCall {
+    int dtype;
+    const void* x;             // [rows][dim]
+    int64_t ldx;
+    const void* w;             // [classes][dim]
+    int64_t ldw;
+    const float* bias;         // [classes] or null
+    int64_t rows, dim, classes;
+    const int32_t* targets;
+    void* work;
+};
+struct ClassifierOut { float *log_prob, *entropy, *lse; };
+struct ClassifierGrads {
+    const float *lse, *entropy, *dlog_prob, *dentropy;
+    void* dx;                  // [rows][dim]
+    int64_t lddx;
+    float* dw;                 // [classes][dim]
+    int64_t lddw;
+    float* dbias;              // [classes] or null
+};
+// for operands that lie as x and w do; null ones: however they lie
+size_t classifier_work_bytes(const ClassifierCall& c, bool backward);
+void launch_classifier(const ClassifierCall& c, const ClassifierOut& out, hipStream_t st);
+void launch_classifier_grads(const ClassifierCall& c, const ClassifierGrads& d, hipStream_t st);
+
 }  // namespace edl

@@ -59,6 +59,36 @@ __device__ __forceinline__ float softmax_entropy(const SoftmaxSums& a) { return 
 // the largest logit, not from lse: exact to a step of its own size, not of the logit's.)
 __device__ __forceinline__ float softmax_log_prob(const SoftmaxSums& a, float z) { return a.s == 0.f ? -INFINITY : (z - a.m) - log2f(a.s) * kLn2; }
 
+// ---- the gradient of a logit ---------------------------------------------------------------------------------------------
+// What a row's logits need: dz = g (1[c = t] - p) - h p (log p + H).
+struct RowFacts {              // of each row; null: none (targets), zeros (gradients)
+    const int32_t* targets;
+    const float *lse, *entropy, *dlog_prob, *dentropy;
+};
+struct LogitGrad {
+    float g, h, lse, both;
+    int64_t target;            // -1: none
+    bool none;                 // zeros, whatever the logits are
+
+    __device__ __forceinline__ float of(float z, bool hot) const {
+        const float lp = z - lse, p = exp2_of(lp * kLog2e);
+        const float d = z == -INFINITY ? 0.f : p * (both - h * fmaxf(lp, kFarBelow));
+        return none ? 0.f : hot ? d + g : d;
+    }
+};
+__device__ __forceinline__ LogitGrad logit_grad(const RowFacts& f, int64_t row, int64_t classes) {
+    LogitGrad r;
+    const int32_t t = f.targets != nullptr ? f.targets[row] : -1;
+    const bool has = t >= 0 && t < classes;
+    r.target = has ? t : -1;
+    r.g = has && f.dlog_prob != nullptr ? f.dlog_prob[row] : 0.f;
+    r.h = f.dentropy != nullptr ? f.dentropy[row] : 0.f;
+    r.lse = f.lse[row];
+    r.both = -(r.g + (r.h != 0.f ? r.h * f.entropy[row] : 0.f));
+    r.none = r.g == 0.f && r.h == 0.f;
+    return r;
+}
+
 // ---- the k largest of a row, one per lane of a wave, best first -------------------------------------------------------
 // Ordered by value, then by the lower class: both in one 64-bit key, so that the result does not depend on the order in
 // which classes come.  -0 and +0 are equal; a NaN ranks as -inf.  Key 0 is no class.

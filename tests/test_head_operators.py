@@ -335,6 +335,243 @@ def test_log_probs_of_no_rows(E):
     assert E.edl_log_probs_backward(z, t, r.lse, r.entropy, r.lse, r.lse).shape == (0, 7)
 
 
+# ---------------------------------------------------------------- classifier
+# Per element, of float32 sums of n products whose errors do not all point one way: 2^-24 (sqrt(n) + 4) sum |a b|.  z: that of
+# its own sum.  dz: p's relative error is z - lse's absolute one.  dx in bf16: dz as two bf16 numbers (2^-16) and half a step.
+def classifier_case(seed, dtype, rows, dim, classes, bias=True, pads=(0, 0), offsets=(0, 0), size=1.0):
+    gen = torch.Generator().manual_seed(seed)
+    x, _ = rows_of(gen, rows, dim, pads[0], dtype, size, offsets[0])
+    w, _ = rows_of(gen, classes, dim, pads[1], dtype, size * (2.0 / dim) ** 0.5, offsets[1])
+    b = torch.randn(classes, generator=gen) * 0.3 if bias else None
+    t = targets_of(gen, rows, classes)
+    return x, w, b, t, gen
+
+
+def classifier_reference(x, w, b, t):
+    xc, wc = x.cpu().double(), w.cpu().double()
+    z = xc @ wc.t() + (0 if b is None else b.double())
+    spread = (xc.abs() @ wc.abs().t() + (0 if b is None else b.double().abs())).max()
+    tol = 2.0 ** -24 * (x.shape[1] ** 0.5 + 4) * float(torch.nan_to_num(spread, posinf=0.0)) + stat_tolerance(z, z.shape[1])
+    return z, R.log_probs(z, t), tol
+
+
+def check_classifier_grads(E, x, w, b, t, r, z, tol, g, h, **kw):
+    rows, dim = x.shape
+    dev = lambda v: None if v is None else v.cuda()         # noqa: E731
+    dx, dw, db = E.edl_classifier_log_probs_backward(x, w, dev(b), dev(t), r.lse, r.entropy, dev(g), dev(h), **kw)
+    dz = R.log_probs_backward(z, t, g, h)
+    xc, wc = x.cpu().double(), w.cpu().double()
+    size = torch.zeros(rows, dtype=torch.float64)
+    if g is not None:
+        size = size + torch.where((t >= 0) & (t < z.shape[1]), g.abs().double(), size)
+    lp = z - torch.logsumexp(z, 1)[:, None]
+    p = lp.exp()
+    # |dz|'s parts before they cancel
+    parts = size[:, None] * p + dz.abs()
+    if h is not None:
+        parts = parts + h.abs().double()[:, None] * p * (lp.abs().clamp(max=1e3) + 15)
+    e = 2 * tol
+    two = 2.0 ** -16 if x.dtype == torch.bfloat16 else 0.0
+    sums = lambda n: 2.0 ** -24 * (n ** 0.5 + 6)            # noqa: E731
+    want = dz @ wc
+    assert bool(((dx.cpu().double() - want).abs() <= (parts @ wc.abs()) * (e + two + sums(z.shape[1])) + R.EPS[x.dtype] * want.abs() + 1e-37).all())
+    want = dz.t() @ xc
+    assert dw.dtype == torch.float32
+    assert bool(((dw.cpu().double() - want).abs() <= (parts.t() @ xc.abs()) * (e + sums(rows)) + 1e-37).all())
+    if b is not None or kw.get("dbias") is not None:
+        assert bool(((db.cpu().double() - dz.sum(0)).abs() <= parts.sum(0) * (e + sums(rows)) + 1e-37).all())
+    return dx, dw, db
+
+
+CLASSIFIERS = [  # rows, dim, classes, bias, pads, offsets
+    (1, 1, 1, True, (0, 0), (0, 0)), (1, 16, 2, False, (0, 0), (0, 0)), (3, 7, 5, True, (1, 2), (1, 0)), (8, 64, 10, True, (0, 0), (0, 0)),
+    (33, 100, 40, True, (0, 0), (0, 0)), (8, 4096, 1000, True, (0, 0), (0, 0)), (256, 512, 1000, True, (0, 0), (0, 0)), (130, 72, 129, False, (8, 8), (0, 0)),
+    (65, 1000, 333, True, (0, 0), (8, 0)), (1, 256, 20000, True, (0, 0), (0, 0)), (2, 48, 24000, True, (0, 3), (0, 0)), (5000, 24, 12, True, (0, 0), (0, 0)),
+    # tiles enough for the sums of whole tiles
+    (300, 64, 8300, True, (0, 0), (0, 0)), (129, 200, 12500, False, (0, 0), (0, 0)), (257, 33, 8192, True, (0, 0), (0, 0)), (1, 40, 24600, True, (0, 0), (0, 0)),
+    (3300, 16, 1000, True, (8, 0), (0, 8)), (640, 130, 5121, True, (0, 0), (1, 1)), (24700, 8, 100, True, (0, 0), (0, 0)), (1030, 320, 3000, True, (0, 0), (0, 0))]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,dim,classes,bias,pads,offsets", CLASSIFIERS)
+def test_classifier_log_probs(E, dtype, rows, dim, classes, bias, pads, offsets):
+    x, w, b, t, _ = classifier_case(rows + dim, dtype, rows, dim, classes, bias, pads, offsets)
+    z, want, tol = classifier_reference(x, w, b, t)
+    dev = lambda v: None if v is None else v.cuda()         # noqa: E731
+    r = E.edl_classifier_log_probs(x, w, dev(b), t.cuda())
+    check_stats(r, want, tol, 0)
+    again = E.edl_classifier_log_probs(x, w, dev(b), t.cuda())
+    assert all(torch.equal(a, c) for a, c in zip(r[:3], again[:3]))
+    q = E.edl_classifier_log_probs(x, w, dev(b))
+    assert q.log_prob is None and torch.equal(q.lse, r.lse) and torch.equal(q.entropy, r.entropy)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,dim,classes,bias,pads,offsets", CLASSIFIERS)
+def test_classifier_backward(E, dtype, rows, dim, classes, bias, pads, offsets):
+    x, w, b, t, gen = classifier_case(rows + dim + 1, dtype, rows, dim, classes, bias, pads, offsets)
+    z, want, tol = classifier_reference(x, w, b, t)
+    dev = lambda v: None if v is None else v.cuda()         # noqa: E731
+    r = E.edl_classifier_log_probs(x, w, dev(b), t.cuda())
+    g, h = torch.randn(rows, generator=gen), torch.randn(rows, generator=gen) * 0.3
+    first = check_classifier_grads(E, x, w, b, t, r, z, tol, g, h)
+    again = check_classifier_grads(E, x, w, b, t, r, z, tol, g, h)
+    assert all(a is None or torch.equal(a, c) for a, c in zip(first, again))
+    check_classifier_grads(E, x, w, b, t, r, z, tol, g, None)
+    check_classifier_grads(E, x, w, b, t, r, z, tol, None, h)
+
+
+def test_classifier_backward_in_several_pieces_of_the_classes(E):
+    """dz of 4,100 rows by 11,003 classes in bf16 is more than is held at a time: two pieces, the second of another size."""
+    rows, dim, classes = 4100, 24, 11003
+    x, w, b, t, gen = classifier_case(31, "bf16", rows, dim, classes)
+    assert rows * classes * 6 > 256 << 20
+    z, want, tol = classifier_reference(x, w, b, t)
+    r = E.edl_classifier_log_probs(x, w, b.cuda(), t.cuda())
+    check_stats(r, want, tol, 0)
+    check_classifier_grads(E, x, w, b, t, r, z, tol, torch.randn(rows, generator=gen), torch.randn(rows, generator=gen) * 0.3)
+
+
+def test_classifier_outputs_in_wider_matrices(E):
+    """Gradients into views of wider matrices: what lies beside their rows stays."""
+    x, w, b, t, gen = classifier_case(5, "bf16", 70, 40, 300)
+    r = E.edl_classifier_log_probs(x, w, b.cuda(), t.cuda())
+    g = torch.randn(70, generator=gen).cuda()
+    plain = E.edl_classifier_log_probs_backward(x, w, b.cuda(), t.cuda(), r.lse, r.entropy, g)
+    bx, bw = torch.full((70, 43), 7.0, device="cuda", dtype=torch.bfloat16), torch.full((300, 47), 7.0, device="cuda")
+    bb = torch.full((302,), 7.0, device="cuda")
+    E.edl_classifier_log_probs_backward(x, w, b.cuda(), t.cuda(), r.lse, r.entropy, g, dx=bx[:, 1:41], dw=bw[:, 2:42], dbias=bb[1:301])
+    assert torch.equal(bx[:, 1:41], plain[0]) and torch.equal(bw[:, 2:42], plain[1]) and torch.equal(bb[1:301], plain[2])
+    assert bool((bx[:, 0] == 7).all() and (bx[:, 41:] == 7).all() and (bw[:, :2] == 7).all() and (bw[:, 42:] == 7).all() and bb[0] == 7 and bb[301] == 7)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,dim,classes", [(40, 64, 500), (300, 64, 8300)])
+def test_classifier_masked_classes_and_rows_that_count_for_nothing(E, dtype, rows, dim, classes):
+    """A bias of -inf takes a class out; targets that are no class; rows with zero gradients leave no trace."""
+    x, w, b, t, gen = classifier_case(9, dtype, rows, dim, classes)
+    b[::3] = -float("inf")
+    t = torch.where(t % 3 == 0, t + 1, t)
+    t[0], t[1], t[2] = classes, -7, 2 ** 31 - 1
+    z, want, tol = classifier_reference(x, w, b, t)
+    r = E.edl_classifier_log_probs(x, w, b.cuda(), t.cuda())
+    check_stats(r, want, tol, 0)
+    assert r.log_prob[:3].tolist() == [0.0, 0.0, 0.0]
+    g, h = torch.randn(rows, generator=gen), torch.randn(rows, generator=gen)
+    g[5:9] = 0
+    h[5:9] = 0
+    dx, dw, db = check_classifier_grads(E, x, w, b, t, r, torch.where(z == -float("inf"), torch.full_like(z, -1e4), z), tol, g, h)
+    assert bool((dx[5:9] == 0).all() and (dw[::3] == 0).all() and (db[::3] == 0).all())
+    everything = torch.full((classes,), -float("inf"))
+    r = E.edl_classifier_log_probs(x, w, everything.cuda(), t.cuda())
+    assert bool((r.lse == -float("inf")).all() and (r.entropy == 0).all())
+    dx, dw, db = E.edl_classifier_log_probs_backward(x, w, everything.cuda(), t.cuda(), r.lse, r.entropy, None, h.cuda())
+    assert bool((dx == 0).all() and (dw == 0).all() and (db == 0).all())
+
+
+def test_classifier_is_log_probs_of_its_logits(E):
+    """The same head with and without logits in memory, and finite differences of the loss along a random direction."""
+    x, w, b, t, gen = classifier_case(13, "f32", 50, 96, 700)
+    r = E.edl_classifier_log_probs(x, w, b.cuda(), t.cuda())
+    z = (x.double() @ w.double().t() + b.cuda().double())
+    q = E.edl_log_probs(z.float(), t.cuda())
+    for a, c in zip(r[:3], q[:3]):
+        assert float((a - c).abs().max()) <= 2e-5
+    g, h = torch.randn(50, generator=gen).cuda(), torch.randn(50, generator=gen).cuda()
+    dx, dw, db = E.edl_classifier_log_probs_backward(x, w, b.cuda(), t.cuda(), r.lse, r.entropy, g, h)
+    ux, uw, ub = (torch.randn(*v.shape, generator=gen).double() for v in (x, w, b))
+
+    def loss(s):
+        zz = (x.cpu().double() + s * ux) @ (w.cpu().double() + s * uw).t() + b.double() + s * ub
+        lp, H, *_ = R.log_probs(zz, t)
+        return float((g.cpu().double() * lp + h.cpu().double() * H).sum())
+    slope = (loss(1e-6) - loss(-1e-6)) / 2e-6
+    mine = float((dx.cpu().double() * ux).sum() + (dw.cpu().double() * uw).sum() + (db.cpu().double() * ub).sum())
+    assert abs(slope - mine) <= 1e-4 * max(1.0, abs(slope))
+
+
+def test_classifier_in_a_replayed_graph_and_on_another_stream(E):
+    x, w, b, t, gen = classifier_case(17, "bf16", 300, 64, 8300)
+    b, t, g = b.cuda(), t.cuda(), torch.randn(300, generator=gen).cuda()
+
+    def call(stream=None):
+        r = E.edl_classifier_log_probs(x, w, b, t, stream=stream)
+        return (*r[:3], *E.edl_classifier_log_probs_backward(x, w, b, t, r.lse, r.entropy, g, g, stream=stream))
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    on_side = call(side.cuda_stream)
+    side.synchronize()
+    for a, c in zip(on_side, call()):
+        assert torch.equal(a, c)
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = call()
+    for i in range(3):
+        x.copy_(torch.randn(300, 64, generator=gen).to(x.dtype).cuda())
+        want = call()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, c in zip(held, want):
+            assert torch.equal(a, c), i
+
+
+def test_classifier_workspace_from_the_caller(E):
+    x, w, b, t, gen = classifier_case(19, "f32", 300, 30, 8300)
+    need = E.edl_classifier_workspace(x, w), E.edl_classifier_workspace(x, w, backward=True)
+    assert min(need) > 0
+    work = torch.full((max(need),), 255, dtype=torch.uint8, device="cuda")       # NaN all over
+    r = E.edl_classifier_log_probs(x, w, b.cuda(), t.cuda(), work=work)
+    want = E.edl_classifier_log_probs(x, w, b.cuda(), t.cuda())
+    assert all(torch.equal(a, c) for a, c in zip(r[:3], want[:3]))
+    work.fill_(255)
+    g = torch.randn(300, generator=gen).cuda()
+    a = E.edl_classifier_log_probs_backward(x, w, b.cuda(), t.cuda(), r.lse, r.entropy, g, work=work)
+    c = E.edl_classifier_log_probs_backward(x, w, b.cuda(), t.cuda(), r.lse, r.entropy, g)
+    assert all(torch.equal(p, q) for p, q in zip(a, c))
+    with pytest.raises(E.EdlError) as ei:
+        E.edl_classifier_log_probs(x, w, b.cuda(), t.cuda(), work=work[:need[0] - 1])
+    assert ei.value.code == -3
+
+
+def test_classifier_of_no_rows(E):
+    x, w = torch.empty(0, 24, device="cuda"), torch.randn(10, 24, device="cuda")
+    t, e = torch.empty(0, dtype=torch.int32, device="cuda"), torch.empty(0, device="cuda")
+    assert E.edl_classifier_log_probs(x, w, None, t).lse.shape == (0,)
+    dx, dw, db = E.edl_classifier_log_probs_backward(x, w, torch.zeros(10, device="cuda"), t, e, e, e, e)
+    assert dx.shape == (0, 24) and bool((dw == 0).all()) and bool((db == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_head_as_it_is_trained(E, dtype):
+    """The operators together: dropout of hidden features, the loss over many classes, its gradient back through the dropout,
+    and the update of the weights (Adam, with its bf16 copy), against the same in float64."""
+    x, w, b, t, gen = classifier_case(23, dtype, 96, 64, 9000)
+    master = w.float().contiguous() if dtype == "bf16" else w
+    n = 9000 * 64
+    m, s = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    key = E.edl_dropout_key(1, 2, 3)
+    y = E.edl_dropout(x, 0.25, key)
+    r = E.edl_classifier_log_probs(y, w, b.cuda(), t.cuda())
+    g = torch.full((96,), -1.0 / 96)
+    z, want, tol = classifier_reference(y, w, b, t)
+    check_stats(r, want, tol, 0)
+    dy, dw, db = check_classifier_grads(E, y, w, b, t, r, z, tol, g, None)
+    dx = E.edl_dropout(dy, 0.25, key)
+    assert same_bits(dx, R.dropout(dy.cpu(), 0.25, key))
+    assert bool((dx[~torch.from_numpy(R.kept(96, 64, 0.25, key)).cuda()] == 0).all())
+    before = master.cpu().double().flatten()
+    w16 = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    E.edl_adam_update([dw.flatten()], master.view(-1), m, s, w16, 0.01, 0.9, 0.999, 1e-8, 0.0, 1)
+    step = 0.01 * torch.sign(dw.cpu().double().flatten()) * (dw.cpu().double().flatten().abs() / (dw.cpu().double().flatten().abs() + 1e-8))
+    # the first step of Adam: lr g / (|g| + eps); half a step of the weight, and the moments' roundings (a few 2^-24 of lr)
+    assert bool(((master.cpu().double().flatten() - (before - step)).abs() <= 2.0 ** -24 * before.abs() + 2e-7).all())
+    assert same_bits(w16, master.flatten().to(torch.bfloat16))
+
+
 # ---------------------------------------------------------------- dropout inside a job
 def _net(model, arch, x, params, table, masks, rate, stored):
     """Logits of MLP, VGG and AlexNet jobs in float64 on the CPU; masks: which elements the hidden layers keep.  Activations

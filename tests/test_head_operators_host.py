@@ -103,3 +103,52 @@ def test_parts_of_a_row_cover_it(E):
         for classes in (1, 8, 1024, 1025, 4096, 4097, 8193, 49999, 200000, 262145, 10 ** 7):
             n = E.edl_log_probs_workspace(rows, classes, 0)
             assert n % (16 * rows) == 0 and n // (16 * rows) <= 64 and n // (16 * rows) != 1
+
+
+CLASSIFIER = dict(dtype=0, x=SOME, ldx=64, w=SOME, ldw=64, b=SOME, rows=4, dim=64, classes=100, t=SOME, lp=SOME, ent=SOME, lse=SOME, work=SOME, bytes=1 << 30)
+CLASSIFIER_BAD = [
+    (dict(dtype=2), -1), (dict(x=None), -1), (dict(w=None), -1), (dict(ldx=63), -1), (dict(ldw=63), -1), (dict(rows=-1), -1), (dict(dim=0), -1),
+    (dict(classes=0), -1), (dict(lse=None), -1), (dict(b=SOME + 2), -1), (dict(t=SOME + 1), -1), (dict(x=SOME + 2), -1), (dict(work=None), -1),
+    (dict(work=SOME + 16), -1), (dict(bytes=16), -3), (dict(rows=2 ** 23 + 1), -4), (dict(dim=2 ** 16 + 1, ldx=2 ** 17, ldw=2 ** 17), -4),
+    (dict(classes=2 ** 24 + 1), -4), (dict(rows=2 ** 16, dim=2 ** 16, ldx=2 ** 16, ldw=2 ** 16), -4), (dict(rows=2 ** 22, classes=2 ** 24), -4),
+    (dict(classes=2 ** 22, dim=2 ** 13, ldx=2 ** 13, ldw=2 ** 13), -4)]
+
+
+@pytest.mark.parametrize("change,code", CLASSIFIER_BAD + [(dict(lp=None), -1), (dict(ent=None), -1)])
+def test_classifier_refusals(E, change, code):
+    a = dict(CLASSIFIER)
+    a.update(change)
+    rc = E.lib.edl_classifier_log_probs(a["dtype"], a["x"], a["ldx"], a["w"], a["ldw"], a["b"], a["rows"], a["dim"], a["classes"], a["t"], a["lp"],
+                                        a["ent"], a["lse"], a["work"], a["bytes"], None)
+    assert rc == code and E.lib.edl_last_error()
+
+
+@pytest.mark.parametrize("change,code", CLASSIFIER_BAD + [
+    (dict(t=None), -1), (dict(ent=None), -1), (dict(dx=None), -1), (dict(lddx=63), -1), (dict(dw=None), -1), (dict(lddw=63), -1), (dict(dw=SOME + 2), -1),
+    (dict(db=SOME + 1), -1), (dict(rows=0, dw=None), -1)])
+def test_classifier_backward_refusals(E, change, code):
+    a = dict(CLASSIFIER, g=SOME, h=SOME, dx=SOME, lddx=64, dw=SOME, lddw=64, db=SOME)
+    if "ldx" in change and change["ldx"] > 64:
+        a.update(lddx=change["ldx"], lddw=change["ldx"])
+    a.update(change)
+    rc = E.lib.edl_classifier_log_probs_backward(a["dtype"], a["x"], a["ldx"], a["w"], a["ldw"], a["b"], a["rows"], a["dim"], a["classes"], a["t"], a["lse"],
+                                                 a["ent"], a["g"], a["h"], a["dx"], a["lddx"], a["dw"], a["lddw"], a["db"], a["work"], a["bytes"], None)
+    assert rc == code and E.lib.edl_last_error()
+
+
+def test_classifier_workspace_grows_with_what_it_holds(E):
+    def need(x, ldx, w, ldw, rows, dim, classes, backward, dtype=1):
+        n = C.c_int64()
+        assert E.lib.edl_classifier_workspace(dtype, x, ldx, w, ldw, rows, dim, classes, backward, C.byref(n)) == 0
+        return n.value
+    aligned = need(SOME, 1024, SOME, 1024, 4096, 1024, 32768, 1)
+    assert aligned <= (256 << 20) + 8 * 4096 * 1024 * 4 + (1 << 20)             # dz a piece at a time, and the pieces' dx
+    copied = need(SOME + 2, 1024, SOME, 1025, 4096, 1024, 32768, 1)
+    assert copied == aligned + 2 * 1024 * (4096 + 32768) == need(None, 0, None, 0, 4096, 1024, 32768, 1)
+    assert need(SOME, 1024, SOME, 1024, 4096, 1024, 32768, 0) < 20 << 20
+    assert need(SOME, 1024, SOME, 1024, 0, 1024, 32768, 1) == 0
+    for rows in (1, 31, 500, 4097):
+        for classes in (1, 100, 5000, 100001):
+            for dim in (1, 64, 4096):
+                for dtype in (0, 1):
+                    assert need(None, 0, None, 0, rows, dim, classes, 0, dtype) > 0 and need(None, 0, None, 0, rows, dim, classes, 1, dtype) > 0
