@@ -14,6 +14,7 @@
 // read it: in float32 as it is, in bf16 as a sum of three bf16 numbers (24 bits), because dw is float32 and a single
 // rounding of dz would be its largest error by four orders of magnitude; dx, which is rounded to bf16, takes the first two.
 #include <algorithm>
+#include <type_traits>
 
 #include "operators.h"
 #include "profiler.h"
@@ -30,7 +31,7 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 
 constexpr int kStepBytes = 128;        // of a reduction step along a row
-constexpr int kTile = 128;             // rows and columns of a block's tile
+constexpr int kTile = 128, kBigTile = 256;     // rows and columns of a block's tile
 
 // ---- operands ---------------------------------------------------------------------------------------------------------
 // 16 bytes per lane from memory to LDS: lane l's go to lds_wave_base + 16 l; lanes whose offset lies past the descriptor's
@@ -143,30 +144,28 @@ template <typename T> __device__ __forceinline__ float fragment_sum(const uint4&
 // row of a 32x32 tile that element e of a lane's 16 stands for (its column is lane % 32)
 __device__ __forceinline__ int tile_row(int e, int lane) { return 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3); }
 
-// x as a sum of bf16 numbers, the first `n` of them: 8 bits each
-template <int N> __device__ __forceinline__ void split_bf16(const float (&v)[4], uint2 (&out)[N]) {
-    float r[4] = {v[0], v[1], v[2], v[3]};
-#pragma unroll
-    for (int q = 0; q < N; ++q) {
-        out[q] = make_uint2(pack2_bf16(r[0], r[1]), pack2_bf16(r[2], r[3]));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) r[e] -= bf16_to_f32((bf16_t)((e < 2 ? out[q].x : out[q].y) >> (16 * (e & 1))));
-    }
+// the next of the bf16 numbers that four floats are the sums of, 8 bits each; what is left of them stays in v
+__device__ __forceinline__ uint2 next_bf16(float (&v)[4]) {
+    const uint2 b = make_uint2(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]));
+    v[0] -= __uint_as_float(b.x << 16);
+    v[1] -= __uint_as_float(b.x & 0xffff0000u);
+    v[2] -= __uint_as_float(b.y << 16);
+    v[3] -= __uint_as_float(b.y & 0xffff0000u);
+    return b;
 }
-
-enum Want { SUMS, GRADS, PRODUCT };     // of z: sums over classes, dz; of the others: the product itself
 
 // four neighbouring classes of a row of dz
 template <typename T> __device__ __forceinline__ void store_dz(char* p, int64_t plane, const float (&d)[4]) {
     if constexpr (sizeof(T) == 4) {
         *reinterpret_cast<float4*>(p) = make_float4(d[0], d[1], d[2], d[3]);
     } else {
-        uint2 parts[3];
-        split_bf16(d, parts);
+        float v[4] = {d[0], d[1], d[2], d[3]};
 #pragma unroll
-        for (int q = 0; q < 3; ++q) *reinterpret_cast<uint2*>(p + q * plane) = parts[q];
+        for (int q = 0; q < 3; ++q) *reinterpret_cast<uint2*>(p + q * plane) = next_bf16(v);
     }
 }
+
+enum Want { SUMS, GRADS, PRODUCT };     // of z: sums over classes, dz; of the others: the product itself
 
 struct GemmArgs {
     Operand a, b;
@@ -207,18 +206,24 @@ __device__ __forceinline__ void tile_of(const GemmArgs& g, int& tm, int& tn, int
     tm = (int)(first + l - (unsigned)tn * high);
 }
 
-template <typename T, Want WANT, bool A_ALONG, bool B_ALONG, typename OUT>
-__global__ __launch_bounds__(256) void gemm_kernel(GemmArgs g) {
-    constexpr int THREADS = 256, TM = 2, TN = 2;           // waves 2 x 2, each 64x64
-    typedef Tile<T, A_ALONG, kTile, THREADS> TA;
-    typedef Tile<T, B_ALONG, kTile, THREADS> TB;
+// A block's waves, WM x WN, and a wave's 32x32 tiles, TM x TN.  64x64 to a wave read 4 KB of LDS for every 4 matrix
+// instructions, 128x64 read 6 KB for 8; what the larger tile needs is enough of them for the chip.
+struct Shape128 { static constexpr int WM = 2, WN = 2, TM = 2, TN = 2; };
+struct Shape256 { static constexpr int WM = 2, WN = 4, TM = 4, TN = 2; };
+
+template <typename T, Want WANT, bool A_ALONG, bool B_ALONG, typename OUT, typename SHAPE>
+__global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmArgs g) {
+    constexpr int WM = SHAPE::WM, WN = SHAPE::WN, TM = SHAPE::TM, TN = SHAPE::TN, THREADS = WM * WN * 64;
+    constexpr int MT = WM * TM * 32, NT = WN * TN * 32;
+    typedef Tile<T, A_ALONG, MT, THREADS> TA;
+    typedef Tile<T, B_ALONG, NT, THREADS> TB;
     constexpr int STAGE = TA::BYTES + TB::BYTES, STEP = TA::STEP;
     __shared__ __attribute__((aligned(16))) char smem[2 * STAGE];
     const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
     int tm, tn, cut;
     tile_of(g, tm, tn, cut);
-    const int64_t m0 = (int64_t)tm * kTile, n0 = (int64_t)tn * kTile;
+    const int64_t m0 = (int64_t)tm * MT, n0 = (int64_t)tn * NT;
     TA ta;
     TB tb;
     ta.init(g.a, m0, g.a_row_bytes);
@@ -243,31 +248,42 @@ __global__ __launch_bounds__(256) void gemm_kernel(GemmArgs g) {
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
     float a_sum[TM] = {};
     const bool sum_a = WANT == PRODUCT && g.dbias != nullptr && tn == 0 && wn == 0;
-    // two stages of LDS: while one is contracted the loads of the next are in flight
-    if (all > 0) load(0);
-    for (int t = 0; t < all; ++t) {
-        wait_loads<0>();
-        __syncthreads();           // this step is there for all waves, and all are done with the stage that is filled now
-        if (t + 1 < all) load((t + 1) & 1);
-        const char* const A = smem + (t & 1) * STAGE;
-        const char* const B = A + TA::BYTES;
+    // two stages of LDS: while one is contracted the loads of the next are in flight; fragments are read one group of
+    // instructions ahead (the barriers keep the compiler from moving them back)
+    auto contract_all = [&](auto with_sum) {
+        if (all > 0) load(0);
+        for (int t = 0; t < all; ++t) {
+            wait_loads<0>();
+            __syncthreads();           // this step is there for all waves, and all are done with the stage that is filled now
+            const char* const A = smem + (t & 1) * STAGE;
+            const char* const B = A + TA::BYTES;
+            uint4 fa[2][TM], fb[2][TN];
+            auto read = [&](int q) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            uint4 fa[TM], fb[TN];
+                for (int i = 0; i < TM; ++i) fa[q & 1][i] = TA::fragment(A, (wm * TM + i) * 32, q, lane);
 #pragma unroll
-            for (int i = 0; i < TM; ++i) fa[i] = TA::fragment(A, (wm * TM + i) * 32, q, lane);
+                for (int j = 0; j < TN; ++j) fb[q & 1][j] = TB::fragment(B, (wn * TN + j) * 32, q, lane);
+            };
+            read(0);
+            if (t + 1 < all) load((t + 1) & 1);
 #pragma unroll
-            for (int j = 0; j < TN; ++j) fb[j] = TB::fragment(B, (wn * TN + j) * 32, q, lane);
+            for (int q = 0; q < 4; ++q) {
+                if (q < 3) read(q + 1);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
+                for (int i = 0; i < TM; ++i)
 #pragma unroll
-                for (int j = 0; j < TN; ++j) multiply<T>(fa[i], fb[j], acc[i][j]);
-            if (WANT == PRODUCT && sum_a) {
+                    for (int j = 0; j < TN; ++j) multiply<T>(fa[q & 1][i], fb[q & 1][j], acc[i][j]);
+                if constexpr (decltype(with_sum)::value) {
 #pragma unroll
-                for (int i = 0; i < TM; ++i) a_sum[i] += fragment_sum<T>(fa[i]);
+                    for (int i = 0; i < TM; ++i) a_sum[i] += fragment_sum<T>(fa[q & 1][i]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
-    }
+    };
+    if (WANT == PRODUCT && sum_a) contract_all(std::true_type{});
+    else contract_all(std::false_type{});
     if constexpr (WANT == PRODUCT) {
         OUT* const out = (OUT*)g.out + cut * g.out_cut;
 #pragma unroll
@@ -303,7 +319,7 @@ __global__ __launch_bounds__(256) void gemm_kernel(GemmArgs g) {
             for (int e = 0; e < 16; ++e) bias[i][e] = g.bias != nullptr && place(i, e) < left ? g.bias[c0 + place(i, e)] : 0.f;
         if constexpr (WANT == SUMS) {
             __syncthreads();                   // LDS is the sums' now
-            float4* const half = reinterpret_cast<float4*>(smem);      // [wm][128]
+            float4* const part = reinterpret_cast<float4*>(smem);      // [wm][NT]
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
                 const int col = (wn * TN + j) * 32 + (lane & 31);
@@ -328,39 +344,69 @@ __global__ __launch_bounds__(256) void gemm_kernel(GemmArgs g) {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) softmax_add(s, acc[i][j][e], base);
                 softmax_join(s, softmax_shuffle(s, 32));
-                if (lane < 32) half[wm * kTile + col] = make_float4(s.m, s.s, s.t, 0.f);
+                if (lane < 32) part[wm * NT + col] = make_float4(s.m, s.s, s.t, 0.f);
                 if (here) g.target_z[n] = zt;
             }
             __syncthreads();
-            if (threadIdx.x < kTile && n0 + threadIdx.x < g.b.rows) {
-                SoftmaxSums s, o;
-                const float4 p = half[threadIdx.x], q = half[kTile + threadIdx.x];
-                s.m = p.x; s.s = p.y; s.t = p.z;
-                o.m = q.x; o.s = q.y; o.t = q.z;
-                softmax_join(s, o);
+            if (threadIdx.x < NT && n0 + threadIdx.x < g.b.rows) {
+                SoftmaxSums s;
+#pragma unroll
+                for (int w = 0; w < WM; ++w) {
+                    const float4 p = part[w * NT + threadIdx.x];
+                    SoftmaxSums o;
+                    o.m = p.x; o.s = p.y; o.t = p.z;
+                    softmax_join(s, o);
+                }
                 g.sums[tm * g.b.rows + n0 + threadIdx.x] = make_float4(s.m, s.s, s.t, 0.f);
             }
         } else {
+            // dz goes out through LDS, a plane at a time, so that rows are written in whole lines: [NT rows][MT classes] with the
+            // 16-byte pieces of a row permuted by its low bits (32 lanes write one piece of 32 rows)
+            constexpr int PLANES = sizeof(T) == 2 ? 3 : 1, PIECES = MT * (int)sizeof(T) / 16;
+            static_assert(NT * MT * (int)sizeof(T) <= 2 * STAGE, "a plane fits");
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
                 const int64_t n = n0 + (wn * TN + j) * 32 + (lane & 31);
-                if (n >= g.b.rows) continue;
-                const LogitGrad row = logit_grad(g.facts, n, g.all_classes);
+                const LogitGrad row = logit_grad(g.facts, min(n, g.b.rows - 1), g.all_classes);
                 const int hot = row.target >= c0 && row.target < c0 + left ? (int)(row.target - c0) : -1;
-                char* const dz = g.dz + n * g.dz_ld + (c0 - g.first_class) * TA::ESZ;
-                const int wide = (int)(g.dz_classes - (c0 - g.first_class));
 #pragma unroll
                 for (int i = 0; i < TM; ++i)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        float d[4];
+                    for (int e = 0; e < 16; ++e) acc[i][j][e] = place(i, e) < left ? row.of(acc[i][j][e] + bias[i][e], place(i, e) == hot) : 0.f;
+            }
+            const int wide = (int)min((int64_t)MT, g.dz_classes - m0) * (int)sizeof(T) / 16;       // pieces of a row that are written
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int at_class = place(i, 4 * q + e);
-                            d[e] = at_class < left ? row.of(acc[i][j][4 * q + e] + bias[i][4 * q + e], at_class == hot) : 0.f;
+            for (int p = 0; p < PLANES; ++p) {
+                __syncthreads();           // LDS is free: of the product's tiles, then of the plane before
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    const int r = (wn * TN + j) * 32 + (lane & 31);
+                    char* const line = smem + r * (MT * (int)sizeof(T));
+#pragma unroll
+                    for (int i = 0; i < TM; ++i)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const int byte = ((wm * TM + i) * 32 + 8 * q + 4 * (lane >> 5)) * (int)sizeof(T);
+                            char* const to = line + (((byte >> 4) ^ (r & (PIECES - 1))) << 4) + (byte & 15);
+                            float d[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) d[e] = acc[i][j][4 * q + e];
+                            if constexpr (sizeof(T) == 4) {
+                                *reinterpret_cast<float4*>(to) = make_float4(d[0], d[1], d[2], d[3]);
+                            } else {
+                                *reinterpret_cast<uint2*>(to) = next_bf16(d);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = d[e];
+                            }
                         }
-                        if (place(i, 4 * q) < wide) store_dz<T>(dz + place(i, 4 * q) * TA::ESZ, g.dz_plane, d);
-                    }
+                }
+                __syncthreads();
+                char* const out = g.dz + p * g.dz_plane + n0 * g.dz_ld + m0 * (int64_t)sizeof(T);
+                for (int s = threadIdx.x; s < NT * PIECES; s += THREADS) {
+                    const int r = s / PIECES, c = s % PIECES;
+                    if (n0 + r < g.b.rows && c < wide)
+                        *reinterpret_cast<uint4*>(out + r * g.dz_ld + c * 16) = *reinterpret_cast<const uint4*>(smem + (r * PIECES + (c ^ (r & (PIECES - 1)))) * 16);
+                }
             }
         }
     }
@@ -569,15 +615,33 @@ __global__ __launch_bounds__(256) void zero_rows_kernel(float* p, int64_t ld, in
 
 constexpr int64_t kMiB = 1 << 20;
 constexpr int64_t kSmallTiles = 192;           // z of fewer tiles is formed in parts (thin_logits_kernel)
-constexpr int64_t kDzBytes = 256 * kMiB;       // of dz at a time: what the last-level cache holds
+constexpr int64_t kDzBytes = 1024 * kMiB;      // of dz at a time
 constexpr int64_t kZeroAtOnce = 1ll << 30;     // elements of dw that one launch clears where there are no rows
 constexpr int64_t kMostAtOnce = 1 << 20;       // classes of it: 64 rows of dz are counted in 32 bits
-constexpr int64_t kWantBlocks = 512;           // two blocks per CU
+constexpr int64_t kWantBlocks = 512;           // two blocks of 128x128 per CU
+constexpr int64_t kChip = 256;                 // CUs: one block of 256x256 each
 constexpr int64_t kWantWaves = 2048;
 constexpr int64_t kThinPart = 4096;            // classes of a part of a row, at least, where rows are few
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
+
+// How a product of M x N outputs over `steps` steps is laid out: tiles of 256x256 where they fill most of the chip, the
+// reduction cut if need be, and little of them hangs over the edges; else of 128x128, the reduction cut towards two blocks
+// per CU, four steps to a cut at least.
+struct Layout { bool big; int cuts, per_cut; };
+Layout lay_out(int64_t M, int64_t N, int64_t steps, int esz, bool may_cut) {
+    Layout l = {};
+    const int64_t big = ceil_div(M, kBigTile) * ceil_div(N, kBigTile), tiles = ceil_div(M, kTile) * ceil_div(N, kTile);
+    const int64_t big_cuts = may_cut && big < kChip ? std::max<int64_t>(1, std::min<int64_t>(kChip / big, steps / 16)) : 1;
+    l.big = esz == 2 && big * big_cuts * 4 >= kChip * 3 && M * N * 4 >= big * kBigTile * kBigTile * 3;
+    int64_t want = 1;
+    if (l.big) want = big_cuts;
+    else if (may_cut && tiles < kWantBlocks / 2) want = std::min<int64_t>(std::max<int64_t>(1, steps / 4), kWantBlocks / tiles);
+    l.per_cut = (int)ceil_div(steps, want);
+    l.cuts = (int)ceil_div(steps, l.per_cut);
+    return l;
+}
 
 // everything a call does, from its sizes and alignments alone
 struct Plan {
@@ -591,18 +655,11 @@ struct Plan {
     int64_t thin_part;
     int planes, dx_planes;
     int64_t chunk, chunks;     // of classes, in the backward pass
-    int dx_cuts, dx_per_cut, dw_cuts, dw_per_cut;
+    Layout z, dx, dw;
+    int64_t z_tiles;           // of classes
     // workspace
     int64_t x_at, w_at, z_at, sums_at, target_at, dz_at, dz_ld, dz_plane, dx_at, dw_at, db_at, bytes;
 };
-
-// cuts of a reduction of `steps` steps where `tiles` blocks are too few: towards kWantBlocks, four steps each at least
-void plan_cuts(int64_t tiles, int64_t steps, int& cuts, int& per_cut) {
-    const int64_t most = std::max<int64_t>(1, steps / 4);
-    const int64_t want = tiles >= kWantBlocks / 2 ? 1 : std::min<int64_t>(most, kWantBlocks / tiles);
-    per_cut = (int)ceil_div(steps, want);
-    cuts = (int)ceil_div(steps, per_cut);
-}
 
 Plan plan_of(int dtype, int64_t rows, int64_t dim, int64_t classes, bool aligned_x, bool aligned_w, bool backward) {
     Plan p = {};
@@ -611,7 +668,7 @@ Plan plan_of(int dtype, int64_t rows, int64_t dim, int64_t classes, bool aligned
     p.wide = round_up(dim, vec);
     p.pad_x = !aligned_x;
     p.pad_w = !aligned_w;
-    const int64_t tiles_r = ceil_div(rows, kTile), tiles_c = ceil_div(classes, kTile), tiles_d = ceil_div(dim, kTile);
+    const int64_t tiles_r = ceil_div(rows, kTile), tiles_c = ceil_div(classes, kTile);
     int64_t o = 0;
     auto take = [&](int64_t bytes) { const int64_t at = o; o += round_up(bytes, 256); return at; };
     p.x_at = take(p.pad_x ? rows * p.wide * p.esz : 0);
@@ -630,7 +687,9 @@ Plan plan_of(int dtype, int64_t rows, int64_t dim, int64_t classes, bool aligned
         p.z_at = take(p.thin_cuts * rows * p.z_ld * 4);
     }
     if (!backward) {
-        p.sums_at = take(p.thin ? (p.thin_parts > 1 ? p.thin_parts * rows * 16 : 0) : tiles_c * rows * 16);
+        p.z = lay_out(classes, rows, 1, p.esz, false);
+        p.z_tiles = ceil_div(classes, p.z.big ? kBigTile : kTile);
+        p.sums_at = take(p.thin ? (p.thin_parts > 1 ? p.thin_parts * rows * 16 : 0) : p.z_tiles * rows * 16);
         p.target_at = take(rows * 4);
     } else {
         p.planes = dtype == 1 ? 3 : 1;
@@ -642,11 +701,13 @@ Plan plan_of(int dtype, int64_t rows, int64_t dim, int64_t classes, bool aligned
         p.dz_ld = round_up(p.chunk * p.esz, 128);
         p.dz_plane = rows * p.dz_ld;
         p.dz_at = take(p.planes * p.dz_plane);
-        plan_cuts(tiles_r * tiles_d, ceil_div(std::min(p.chunk, classes), step), p.dx_cuts, p.dx_per_cut);
-        plan_cuts(ceil_div(std::min(p.chunk, classes), kTile) * tiles_d, ceil_div(rows, step), p.dw_cuts, p.dw_per_cut);
-        p.dx_at = take(p.chunks * p.dx_cuts > 1 ? p.chunks * p.dx_cuts * rows * dim * 4 : 0);
-        p.dw_at = take(p.dw_cuts > 1 ? p.dw_cuts * p.chunk * dim * 4 : 0);
-        p.db_at = take(p.dw_cuts > 1 ? p.dw_cuts * p.chunk * 4 : 0);
+        const int64_t n = std::min(p.chunk, classes);
+        p.z = lay_out(n, rows, 1, p.esz, false);
+        p.dx = lay_out(rows, dim, ceil_div(n, step), p.esz, true);
+        p.dw = lay_out(n, dim, ceil_div(rows, step), p.esz, true);
+        p.dx_at = take(p.chunks * p.dx.cuts > 1 ? p.chunks * p.dx.cuts * rows * dim * 4 : 0);
+        p.dw_at = take(p.dw.cuts > 1 ? p.dw.cuts * p.chunk * dim * 4 : 0);
+        p.db_at = take(p.dw.cuts > 1 ? p.dw.cuts * p.chunk * 4 : 0);
     }
     p.bytes = o;
     return p;
@@ -680,7 +741,7 @@ template <typename T> ThinRows thin_forward(const Operand& x, const Operand& w, 
     return ThinRows{t.z, p.z_ld, x.rows, w.rows, p.thin_cuts, bias, facts};
 }
 
-GemmArgs product_of(const Operand& a, const Operand& b, int64_t a_k, int64_t b_k, int esz) {
+GemmArgs product_of(const Operand& a, const Operand& b, int64_t a_k, int64_t b_k, int esz, bool big) {
     GemmArgs g = {};
     g.a = a;
     g.b = b;
@@ -688,10 +749,21 @@ GemmArgs product_of(const Operand& a, const Operand& b, int64_t a_k, int64_t b_k
     g.b_k = b_k;
     g.planes = 1;
     g.steps = g.steps_per_cut = (int)ceil_div(a_k * esz, kStepBytes);
-    g.tiles_m = (int)ceil_div(a.rows, kTile);
-    g.tiles_n = (int)ceil_div(b.rows, kTile);
-    g.group = 8;
+    g.tiles_m = (int)ceil_div(a.rows, big ? kBigTile : kTile);
+    g.tiles_n = (int)ceil_div(b.rows, big ? kBigTile : kTile);
+    g.group = big ? 4 : 8;
     return g;
+}
+
+template <typename T, Want WANT, bool A_ALONG, bool B_ALONG, typename OUT> void launch_gemm(const GemmArgs& g, int cuts, bool big, hipStream_t st) {
+    const dim3 grid((unsigned)(g.tiles_m * g.tiles_n * cuts));
+    if constexpr (sizeof(T) == 2) {
+        if (big) {
+            hipLaunchKernelGGL((gemm_kernel<T, WANT, A_ALONG, B_ALONG, OUT, Shape256>), grid, dim3(512), 0, st, g);
+            return;
+        }
+    }
+    hipLaunchKernelGGL((gemm_kernel<T, WANT, A_ALONG, B_ALONG, OUT, Shape128>), grid, dim3(256), 0, st, g);
 }
 
 template <typename T> void forward(const ClassifierCall& c, const ClassifierOut& out, hipStream_t st) {
@@ -712,7 +784,7 @@ template <typename T> void forward(const ClassifierCall& c, const ClassifierOut&
         tiles = p.thin_parts;
         if (tiles == 1) return;
     } else {
-        GemmArgs g = product_of(w, x, p.wide, p.wide, p.esz);
+        GemmArgs g = product_of(w, x, p.wide, p.wide, p.esz, p.z.big);
         g.bias = c.bias;
         g.classes = c.classes;
         g.facts = facts;
@@ -720,7 +792,7 @@ template <typename T> void forward(const ClassifierCall& c, const ClassifierOut&
         g.target_z = target_z;
         tiles = g.tiles_m;
         ProfScope ps("classifier_sums", 2.0 * c.rows * c.classes * c.dim, (double)(c.rows + c.classes) * c.dim * p.esz, st);
-        hipLaunchKernelGGL((gemm_kernel<T, SUMS, true, true, float>), dim3((unsigned)(g.tiles_m * g.tiles_n)), dim3(256), 0, st, g);
+        launch_gemm<T, SUMS, true, true, float>(g, 1, p.z.big, st);
     }
     ProfScope ps("classifier_join", 0.0, 16.0 * tiles * c.rows, st);
     hipLaunchKernelGGL(classifier_join_kernel, dim3((unsigned)ceil_div(c.rows, 32)), dim3(256), 0, st, sums, tiles, c.rows, c.targets, c.classes, target_z, res);
@@ -739,7 +811,7 @@ template <typename T> void backward(const ClassifierCall& c, const ClassifierGra
     const Operand w = padded<T>(c.w, c.ldw, c.classes, c.dim, p, p.pad_w, p.w_at, work, st);
     const RowFacts facts = {c.targets, d.lse, d.entropy, d.dlog_prob, d.dentropy};
     char* const dz = work + p.dz_at;
-    const int64_t slots = p.chunks * p.dx_cuts;
+    const int64_t slots = p.chunks * p.dx.cuts;
     const int row_bytes = (int)(p.wide * p.esz);
     for (int64_t q = 0; q < p.chunks; ++q) {
         const int64_t from = q * p.chunk, n = std::min(p.chunk, c.classes - from), cols = round_up(n, 16 / p.esz);
@@ -749,7 +821,7 @@ template <typename T> void backward(const ClassifierCall& c, const ClassifierGra
             ProfScope ps("classifier_thin_grads", 0.0, (4.0 * p.thin_cuts + p.planes * p.esz) * c.rows * c.classes, st);
             hipLaunchKernelGGL((thin_grads_kernel<T>), dim3((unsigned)(c.rows * ceil_div(cols / 4, 256))), dim3(256), 0, st, z, dz, p.dz_ld, p.dz_plane, (int)cols);
         } else {
-            GemmArgs g = product_of(wq, x, p.wide, p.wide, p.esz);
+            GemmArgs g = product_of(wq, x, p.wide, p.wide, p.esz, p.z.big);
             g.bias = c.bias;
             g.first_class = from;
             g.classes = from + n;
@@ -760,41 +832,40 @@ template <typename T> void backward(const ClassifierCall& c, const ClassifierGra
             g.dz_plane = p.dz_plane;
             g.dz_classes = (int)cols;
             ProfScope ps("classifier_dz", 2.0 * c.rows * n * c.dim, (double)(c.rows + n) * c.dim * p.esz + (double)p.planes * p.esz * c.rows * n, st);
-            hipLaunchKernelGGL((gemm_kernel<T, GRADS, true, true, float>), dim3((unsigned)(g.tiles_m * g.tiles_n)), dim3(256), 0, st, g);
+            launch_gemm<T, GRADS, true, true, float>(g, 1, p.z.big, st);
         }
         {
-            GemmArgs g = product_of(Operand{dz, p.dz_ld, c.rows}, Operand{wq.p, wq.ld, c.dim}, cols, n, p.esz);
+            GemmArgs g = product_of(Operand{dz, p.dz_ld, c.rows}, Operand{wq.p, wq.ld, c.dim}, cols, n, p.esz, p.dx.big);
             g.a_plane = p.dz_plane;
             g.planes = p.dx_planes;
             g.b_row_bytes = row_bytes;
-            g.steps_per_cut = p.dx_per_cut;
+            g.steps_per_cut = p.dx.per_cut;
             const int cuts = (int)ceil_div(g.steps, g.steps_per_cut);
             ProfScope ps("classifier_dx", 2.0 * c.rows * n * c.dim, (double)p.dx_planes * p.esz * c.rows * n + (double)p.esz * (n + c.rows) * c.dim, st);
-            const dim3 grid((unsigned)(g.tiles_m * g.tiles_n * cuts));
             if (slots > 1) {
                 // (the last chunk may have fewer cuts: the slots it leaves out are not summed, see below)
-                g.out = (float*)(work + p.dx_at) + q * p.dx_cuts * c.rows * c.dim;
+                g.out = (float*)(work + p.dx_at) + q * p.dx.cuts * c.rows * c.dim;
                 g.out_ld = c.dim;
                 g.out_cut = c.rows * c.dim;
-                hipLaunchKernelGGL((gemm_kernel<T, PRODUCT, true, false, float>), grid, dim3(256), 0, st, g);
+                launch_gemm<T, PRODUCT, true, false, float>(g, cuts, p.dx.big, st);
             } else {
                 g.out = d.dx;
                 g.out_ld = d.lddx;
-                hipLaunchKernelGGL((gemm_kernel<T, PRODUCT, true, false, T>), grid, dim3(256), 0, st, g);
+                launch_gemm<T, PRODUCT, true, false, T>(g, cuts, p.dx.big, st);
             }
             if (q + 1 == p.chunks && slots > 1) {
-                const int64_t used = (p.chunks - 1) * p.dx_cuts + cuts;
+                const int64_t used = (p.chunks - 1) * p.dx.cuts + cuts;
                 sum_slots<T>((const float*)(work + p.dx_at), used, c.rows, c.dim, (T*)d.dx, d.lddx, st);
             }
         }
         {
-            GemmArgs g = product_of(Operand{dz, p.dz_ld, n}, Operand{x.p, x.ld, c.dim}, c.rows, c.rows, p.esz);
+            GemmArgs g = product_of(Operand{dz, p.dz_ld, n}, Operand{x.p, x.ld, c.dim}, c.rows, c.rows, p.esz, p.dw.big);
             g.a_plane = p.dz_plane;
             g.planes = p.planes;
             g.a_row_bytes = (int)(cols * p.esz);
             g.b_row_bytes = row_bytes;
-            g.steps_per_cut = p.dw_per_cut;
-            const bool cut = p.dw_cuts > 1;
+            g.steps_per_cut = p.dw.per_cut;
+            const bool cut = p.dw.cuts > 1;
             g.out = cut ? (float*)(work + p.dw_at) : d.dw + from * d.lddw;
             g.out_ld = cut ? c.dim : d.lddw;
             g.out_cut = n * c.dim;
@@ -804,11 +875,11 @@ template <typename T> void backward(const ClassifierCall& c, const ClassifierGra
             }
             {
                 ProfScope ps("classifier_dw", 2.0 * c.rows * n * c.dim, (double)p.planes * p.esz * c.rows * n + (double)p.esz * c.rows * c.dim + 4.0 * n * c.dim, st);
-                hipLaunchKernelGGL((gemm_kernel<T, PRODUCT, false, false, float>), dim3((unsigned)(g.tiles_m * g.tiles_n * p.dw_cuts)), dim3(256), 0, st, g);
+                launch_gemm<T, PRODUCT, false, false, float>(g, p.dw.cuts, p.dw.big, st);
             }
             if (cut) {
-                sum_slots<float>((const float*)(work + p.dw_at), p.dw_cuts, n, c.dim, d.dw + from * d.lddw, d.lddw, st);
-                if (d.dbias != nullptr) sum_slots<float>((const float*)(work + p.db_at), p.dw_cuts, 1, n, d.dbias + from, n, st);
+                sum_slots<float>((const float*)(work + p.dw_at), p.dw.cuts, n, c.dim, d.dw + from * d.lddw, d.lddw, st);
+                if (d.dbias != nullptr) sum_slots<float>((const float*)(work + p.db_at), p.dw.cuts, 1, n, d.dbias + from, n, st);
             }
         }
     }

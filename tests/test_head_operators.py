@@ -422,12 +422,23 @@ def test_classifier_backward(E, dtype, rows, dim, classes, bias, pads, offsets):
 
 
 def test_classifier_backward_in_several_pieces_of_the_classes(E):
-    """dz of 4,100 rows by 11,003 classes in bf16 is more than is held at a time: two pieces, the second of another size."""
-    rows, dim, classes = 4100, 24, 11003
+    """dz of more rows and classes than are held at a time: two pieces, the second of another size."""
+    rows, dim, classes = 16400, 24, 11003
     x, w, b, t, gen = classifier_case(31, "bf16", rows, dim, classes)
-    assert rows * classes * 6 > 256 << 20
+    assert rows * classes * 6 > 1 << 30
     z, want, tol = classifier_reference(x, w, b, t)
     r = E.edl_classifier_log_probs(x, w, b.cuda(), t.cuda())
+    check_stats(r, want, tol, 0)
+    check_classifier_grads(E, x, w, b, t, r, z, tol, torch.randn(rows, generator=gen), torch.randn(rows, generator=gen) * 0.3)
+
+
+@pytest.mark.parametrize("rows,dim,classes,bias", [(1100, 1024, 13000, True), (1085, 1001, 13003, False)])
+def test_classifier_of_large_tiles(E, rows, dim, classes, bias):
+    """Sizes whose products run on 256x256 tiles, the one for dx with its reduction cut: even ones, and odd ones throughout."""
+    x, w, b, t, gen = classifier_case(37, "bf16", rows, dim, classes, bias)
+    z, want, tol = classifier_reference(x, w, b, t)
+    dev = lambda v: None if v is None else v.cuda()         # noqa: E731
+    r = E.edl_classifier_log_probs(x, w, dev(b), t.cuda())
     check_stats(r, want, tol, 0)
     check_classifier_grads(E, x, w, b, t, r, z, tol, torch.randn(rows, generator=gen), torch.randn(rows, generator=gen) * 0.3)
 
