@@ -11,6 +11,14 @@ import os
 
 import numpy as np
 
+# The caller's device memory and streams come from PyTorch, which ships a HIP runtime of its own.  It has to
+# be the one already in the process when this library is mapped, so that both see the same runtime (a
+# second copy finds no device): torch first, whatever order the caller imports things in.
+try:
+    import torch
+except ImportError:
+    torch = None
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.environ.get("EDL_LIBRARY") or os.path.join(_HERE, "libedl.so")   # EDL_LIBRARY: another build of the same library
 
@@ -47,13 +55,6 @@ def _load():
     if not os.path.exists(_LIB_PATH):
         from . import build as _b
         _b.build()
-    # The caller's device memory and streams come from PyTorch, which ships a HIP runtime of its own.  It has to
-    # be the one already in the process when this library is mapped, so that both see the same runtime (a
-    # second copy finds no device): torch first, whatever order the caller imports things in.
-    try:
-        import torch  # noqa: F401
-    except ImportError:
-        pass
     return C.CDLL(_LIB_PATH)
 
 
@@ -265,64 +266,66 @@ def edl_copy(dst, src, nbytes, stream=0):
 # -- operators of a classifier's head ---------------------------------------------------------------------------------
 # Tensors stay where they are: matrices may be views whose rows lie any number of elements apart.  Work goes to torch's
 # current stream of the tensors' device, or to `stream` (a raw stream handle, 0 the default stream); what a call allocates
-# belongs to that stream.  Wrong arguments raise EdlError, as the library's own checks do.
+# belongs to that stream.  Wrong arguments raise EdlError, as the library's own checks do.  (A small call's time is its host
+# time, about 4 us of it the launch: the checks below ask for as little as they can.)
+
+def _raw_stream(index):
+    return torch.cuda.current_stream(index).cuda_stream
+
+
+if torch is not None and hasattr(torch._C, "_cuda_getCurrentRawStream"):
+    _raw_stream = torch._C._cuda_getCurrentRawStream       # the same number without an object around it (2 us less)
+
 
 def _refuse(msg):
     raise EdlError(-1, msg)
 
 
 def _dtype_of(name, x):
-    code = {"torch.float32": 0, "torch.bfloat16": 1}.get(str(x.dtype))
-    if code is None:
-        _refuse("%s must be float32 or bfloat16, not %s" % (name, x.dtype))
-    return code
+    d = x.dtype
+    if d is torch.float32:
+        return 0
+    if d is torch.bfloat16:
+        return 1
+    _refuse("%s must be float32 or bfloat16, not %s" % (name, d))
 
 
-def _matrix(name, x, shape=None, like=None):
-    """(pointer, elements between rows) of a [rows][cols] tensor on a GPU."""
-    if x.dim() != 2 or (shape is not None and tuple(x.shape) != tuple(shape)):
-        _refuse("%s must be a matrix%s, not %s" % (name, "" if shape is None else " of %d x %d" % tuple(shape), tuple(x.shape)))
+def _matrix(name, x, shape=None, like=None, dtype=None):
+    """(pointer, elements between rows) of a [rows][cols] tensor on a GPU (like's, and of its type unless dtype says another)."""
+    if x.dim() != 2 or (shape is not None and tuple(x.shape) != shape):
+        _refuse("%s must be a matrix%s, not %s" % (name, "" if shape is None else " of %d x %d" % shape, tuple(x.shape)))
     if not x.is_cuda:
         _refuse("%s must be on a GPU" % name)
-    if like is not None and (x.dtype != like.dtype or x.device != like.device):
-        _refuse("%s is %s on %s, expected %s on %s" % (name, x.dtype, x.device, like.dtype, like.device))
+    if like is not None and (x.dtype is not (like.dtype if dtype is None else dtype) or x.device != like.device):
+        _refuse("%s is %s on %s, expected %s on %s" % (name, x.dtype, x.device, like.dtype if dtype is None else dtype, like.device))
     rows, cols = x.shape
-    if cols > 1 and x.stride(1) != 1:
+    step, side = x.stride()
+    if side != 1 and cols > 1:
         _refuse("neighbouring elements of a row of %s must be neighbours in memory" % name)
-    return x.data_ptr(), x.stride(0) if rows > 1 else cols
+    return x.data_ptr(), step if rows > 1 else cols
 
 
-def _vector(name, v, n, dtype, like):
-    """Pointer of a contiguous [n] tensor of that type on like's device; None stays None."""
+def _vector(name, v, n, dtype, device):
+    """Pointer of a contiguous [n] tensor of that type and device; None stays None."""
     if v is None:
         return None
-    if str(v.dtype) != dtype or tuple(v.shape) != (n,) or v.device != like.device or not v.is_contiguous():
-        _refuse("%s must be a contiguous %s vector of %d on %s" % (name, dtype, n, like.device))
+    if v.dtype is not dtype or v.dim() != 1 or v.shape[0] != n or v.device != device or not v.is_contiguous():
+        _refuse("%s must be a contiguous %s vector of %d on %s" % (name, dtype, n, device))
     return v.data_ptr()
 
 
-class _On:
-    """with _On(x, stream) as raw: x's device is current and raw the stream to launch on, which torch allocates for."""
-
-    def __init__(self, x, stream):
-        import torch
-        self._guards = []
-        if torch.cuda.current_device() != x.device.index:
-            self._guards.append(torch.cuda.device(x.device))
-        if stream is not None:
-            given = torch.cuda.ExternalStream(stream, device=x.device) if stream else torch.cuda.default_stream(x.device)
-            self._guards.append(torch.cuda.stream(given))
-        self._torch, self._device = torch, x.device
-
-    def __enter__(self):
-        for g in self._guards:
-            g.__enter__()
-        return self._torch.cuda.current_stream(self._device).cuda_stream
-
-    def __exit__(self, *exc):
-        for g in reversed(self._guards):
-            g.__exit__(*exc)
-        return False
+def _on(x, stream, work):
+    """work(raw stream) with x's device current and, if another stream than torch's current one is given, that one current (torch
+    then allocates for it)."""
+    index = x.device.index
+    if stream is None and torch.cuda.current_device() == index:
+        return work(_raw_stream(index))
+    with torch.cuda.device(index):
+        if stream is None:
+            return work(_raw_stream(index))
+        given = torch.cuda.ExternalStream(stream, device=x.device) if stream else torch.cuda.default_stream(x.device)
+        with torch.cuda.stream(given):
+            return work(stream)
 
 
 def edl_dropout_key(seed, step, layer):
@@ -336,13 +339,14 @@ def edl_dropout(x, rate, key, first_row=0, out=None, stream=None):
     The gradient is the same call on the gradient of the result."""
     dt = _dtype_of("x", x)
     px, ldx = _matrix("x", x)
-    with _On(x, stream) as st:
-        if out is None:
-            import torch
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        py, ldy = _matrix("out", out, x.shape, x)
-        _check(lib.edl_dropout(dt, px, ldx, py, ldy, x.shape[0], x.shape[1], rate, key, first_row, st))
-    return out
+    rows, cols = x.shape
+
+    def work(st):
+        y = x.new_empty((rows, cols)) if out is None else out
+        py, ldy = (y.data_ptr(), cols) if out is None else _matrix("out", out, (rows, cols), x)
+        _check(lib.edl_dropout(dt, px, ldx, py, ldy, rows, cols, rate, key, first_row, st))
+        return y
+    return _on(x, stream, work)
 
 
 # What edl_log_probs and edl_classifier_log_probs give: float32 vectors (log_prob None without targets), and with `top`
@@ -356,44 +360,52 @@ def edl_log_probs_workspace(rows, classes, top=0):
     return n.value
 
 
+def _results(x, rows, targets):
+    """log_prob (None without targets), entropy and lse, new, and their pointers."""
+    f = x.new_empty((3, rows), dtype=torch.float32)
+    base, step = f.data_ptr(), 4 * rows
+    log_prob, entropy, lse = f.unbind(0)
+    return (log_prob if targets is not None else None, entropy, lse), (base if targets is not None else None, base + step, base + 2 * step)
+
+
 def edl_log_probs(logits, targets=None, top=0, stream=None):
     """Log probabilities of the target classes (int32 [rows]; a negative one: none), entropy, log-sum-exp and the `top` most
     likely classes of rows of logits: a LogProbs."""
-    import torch
     dt = _dtype_of("logits", logits)
     pz, ld = _matrix("logits", logits)
     rows, classes = logits.shape
-    pt = _vector("targets", targets, rows, "torch.int32", logits)
+    pt = _vector("targets", targets, rows, torch.int32, logits.device)
     need = edl_log_probs_workspace(rows, classes, top)
-    with _On(logits, stream) as st:
-        # one allocation for the float32 results, one for the rest of a call
-        f = torch.empty((3 + top, rows), dtype=torch.float32, device=logits.device)
-        best = torch.empty((rows, top), dtype=torch.int32, device=logits.device) if top > 0 else None
-        work = torch.empty(need, dtype=torch.uint8, device=logits.device) if need else None
-        r = LogProbs(f[0] if targets is not None else None, f[1], f[2], f[3:].view(rows, top) if top > 0 else None, best)
-        base = f.data_ptr()
-        _check(lib.edl_log_probs(dt, pz, ld, rows, classes, pt, top, base if pt else None, base + 4 * rows, base + 8 * rows,
-                                 base + 12 * rows if top > 0 else None, best.data_ptr() if top > 0 else None,
-                                 work.data_ptr() if need else None, need, st))
-    return r
+
+    def work(st):
+        r, pr = _results(logits, rows, targets)
+        tv = tc = ws = None
+        if top > 0:
+            tv, tc = logits.new_empty((rows, top), dtype=torch.float32), logits.new_empty((rows, top), dtype=torch.int32)
+        if need:
+            ws = logits.new_empty(need, dtype=torch.uint8)
+        _check(lib.edl_log_probs(dt, pz, ld, rows, classes, pt, top, *pr, None if tv is None else tv.data_ptr(), None if tc is None else tc.data_ptr(),
+                                 None if ws is None else ws.data_ptr(), need, st))
+        return LogProbs(*r, tv, tc)
+    return _on(logits, stream, work)
 
 
 def edl_log_probs_backward(logits, targets, lse, entropy, dlog_prob=None, dentropy=None, out=None, stream=None):
     """Gradient of the logits, in their type, for gradients of log_prob and entropy (None: zeros).  out: where it goes (the
     logits themselves: in place)."""
-    import torch
     dt = _dtype_of("logits", logits)
     pz, ld = _matrix("logits", logits)
     rows, classes = logits.shape
-    vec = [_vector(name, v, rows, kind, logits) for name, v, kind in (
-        ("targets", targets, "torch.int32"), ("lse", lse, "torch.float32"), ("entropy", entropy, "torch.float32"),
-        ("dlog_prob", dlog_prob, "torch.float32"), ("dentropy", dentropy, "torch.float32"))]
-    with _On(logits, stream) as st:
-        if out is None:
-            out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-        pd, ldd = _matrix("out", out, logits.shape, logits)
+    device, f32 = logits.device, torch.float32
+    vec = (_vector("targets", targets, rows, torch.int32, device), _vector("lse", lse, rows, f32, device), _vector("entropy", entropy, rows, f32, device),
+           _vector("dlog_prob", dlog_prob, rows, f32, device), _vector("dentropy", dentropy, rows, f32, device))
+
+    def work(st):
+        d = logits.new_empty((rows, classes)) if out is None else out
+        pd, ldd = (d.data_ptr(), classes) if out is None else _matrix("out", out, (rows, classes), logits)
         _check(lib.edl_log_probs_backward(dt, pz, ld, rows, classes, *vec, pd, ldd, st))
-    return out
+        return d
+    return _on(logits, stream, work)
 
 
 def _classifier(x, w, bias, targets):
@@ -402,66 +414,66 @@ def _classifier(x, w, bias, targets):
     rows, dim = x.shape
     pw, ldw = _matrix("w", w, (w.shape[0], dim) if w.dim() == 2 else None, x)
     classes = w.shape[0]
-    pb = _vector("bias", bias, classes, "torch.float32", x)
-    pt = _vector("targets", targets, rows, "torch.int32", x)
-    return dt, px, ldx, pw, ldw, pb, rows, dim, classes, pt
+    return (dt, px, ldx, pw, ldw, _vector("bias", bias, classes, torch.float32, x.device), rows, dim, classes,
+            _vector("targets", targets, rows, torch.int32, x.device))
+
+
+def _classifier_need(args, backward):
+    dt, px, ldx, pw, ldw, _, rows, dim, classes, _ = args
+    n = C.c_int64()
+    _check(lib.edl_classifier_workspace(dt, px, ldx, pw, ldw, rows, dim, classes, backward, C.byref(n)))
+    return n.value
 
 
 def edl_classifier_workspace(x, w, backward=False):
     """Bytes of workspace that edl_classifier_log_probs (or its gradient) of these features and weights takes."""
-    dt, px, ldx, pw, ldw, _, rows, dim, classes, _ = _classifier(x, w, None, None)
-    n = C.c_int64()
-    _check(lib.edl_classifier_workspace(dt, px, ldx, pw, ldw, rows, dim, classes, 1 if backward else 0, C.byref(n)))
-    return n.value
+    return _classifier_need(_classifier(x, w, None, None), 1 if backward else 0)
 
 
-def _workspace(need, work, like):
-    import torch
-    if work is None:
-        return torch.empty(need, dtype=torch.uint8, device=like.device) if need else None
-    if str(work.dtype) != "torch.uint8" or work.device != like.device or not work.is_contiguous():
-        _refuse("the workspace must be a contiguous uint8 tensor on %s" % like.device)
-    return work
+def _workspace(args, backward, given, x):
+    """(tensor or None, pointer, bytes)"""
+    if given is None:
+        need = _classifier_need(args, backward)
+        given = x.new_empty(need, dtype=torch.uint8) if need else None
+    elif given.dtype is not torch.uint8 or given.device != x.device or not given.is_contiguous():
+        _refuse("the workspace must be a contiguous uint8 tensor on %s" % x.device)
+    return (None, None, 0) if given is None else (given, given.data_ptr(), given.numel())
 
 
 def edl_classifier_log_probs(x, w, bias=None, targets=None, work=None, stream=None):
     """edl_log_probs (without alternatives) of the logits x w^T + bias, which are not stored.  x: [rows][dim], w: [classes][dim]
     of the same type, bias: float32 [classes].  work: uint8 workspace (None: a new one)."""
-    import torch
     args = _classifier(x, w, bias, targets)
-    rows = x.shape[0]
-    with _On(x, stream) as st:
-        work = _workspace(edl_classifier_workspace(x, w) if work is None else 0, work, x)
-        f = torch.empty((3, rows), dtype=torch.float32, device=x.device)
-        base = f.data_ptr()
-        _check(lib.edl_classifier_log_probs(*args, base if targets is not None else None, base + 4 * rows, base + 8 * rows,
-                                            None if work is None else work.data_ptr(), 0 if work is None else work.numel(), st))
-    return LogProbs(f[0] if targets is not None else None, f[1], f[2], None, None)
+
+    def call(st):
+        r, pr = _results(x, x.shape[0], targets)
+        held, ws, size = _workspace(args, 0, work, x)
+        _check(lib.edl_classifier_log_probs(*args, *pr, ws, size, st))
+        return LogProbs(*r, None, None)
+    return _on(x, stream, call)
 
 
 def edl_classifier_log_probs_backward(x, w, bias, targets, lse, entropy, dlog_prob=None, dentropy=None, work=None, stream=None,
                                       dx=None, dw=None, dbias=None):
     """(dx, dw, dbias): gradients of the features in their type and of weights and bias in float32 (dbias None without a
     bias), for gradients of log_prob and entropy (None: zeros).  dx, dw, dbias: where they go (None: new tensors)."""
-    import torch
     args = _classifier(x, w, bias, targets)
     rows, dim = x.shape
     classes = w.shape[0]
-    vec = [_vector(name, v, rows, "torch.float32", x) for name, v in (("lse", lse), ("entropy", entropy), ("dlog_prob", dlog_prob), ("dentropy", dentropy))]
-    with _On(x, stream) as st:
-        work = _workspace(edl_classifier_workspace(x, w, True) if work is None else 0, work, x)
-        dx = torch.empty((rows, dim), dtype=x.dtype, device=x.device) if dx is None else dx
-        dw = torch.empty((classes, dim), dtype=torch.float32, device=x.device) if dw is None else dw
-        if bias is not None and dbias is None:
-            dbias = torch.empty(classes, dtype=torch.float32, device=x.device)
-        pdx, lddx = _matrix("dx", dx, (rows, dim), x)
-        pdw, lddw = _matrix("dw", dw, (classes, dim))
-        if str(dw.dtype) != "torch.float32" or dw.device != x.device:
-            _refuse("dw must be float32 on %s" % x.device)
-        pdb = _vector("dbias", dbias, classes, "torch.float32", x)
-        _check(lib.edl_classifier_log_probs_backward(*args, *vec, pdx, lddx, pdw, lddw, pdb, None if work is None else work.data_ptr(),
-                                                     0 if work is None else work.numel(), st))
-    return dx, dw, dbias
+    device, f32 = x.device, torch.float32
+    vec = (_vector("lse", lse, rows, f32, device), _vector("entropy", entropy, rows, f32, device), _vector("dlog_prob", dlog_prob, rows, f32, device),
+           _vector("dentropy", dentropy, rows, f32, device))
+
+    def call(st):
+        held, ws, size = _workspace(args, 1, work, x)
+        gx = x.new_empty((rows, dim)) if dx is None else dx
+        gw = x.new_empty((classes, dim), dtype=f32) if dw is None else dw
+        gb = x.new_empty(classes, dtype=f32) if bias is not None and dbias is None else dbias
+        pdx, lddx = _matrix("dx", gx, (rows, dim), x)
+        pdw, lddw = _matrix("dw", gw, (classes, dim), x, f32)
+        _check(lib.edl_classifier_log_probs_backward(*args, *vec, pdx, lddx, pdw, lddw, _vector("dbias", gb, classes, f32, device), ws, size, st))
+        return gx, gw, gb
+    return _on(x, stream, call)
 
 
 def edl_set_option(name, value):

@@ -40,8 +40,8 @@ constexpr int kTile = 128, kBigTile = 256;     // rows and columns of a block's 
 constexpr unsigned kNowhere = 0x80000000u;       // past any extent (they are clamped below it)
 __device__ __forceinline__ i32x4 extent_of(const char* p, int64_t bytes) {
     const uint64_t a = (uint64_t)p;
-    const int n = bytes <= 0 ? 0 : bytes > 0x7ffffff0 ? 0x7ffffff0 : (int)bytes;
-    const i32x4 r = {(int)(uint32_t)a, (int)((uint32_t)(a >> 32) & 0xffffu), n, 0x00020000};
+    auto same = [](int v) { return __builtin_amdgcn_readfirstlane(v); };       // (they are: the compiler has lost track)
+    const i32x4 r = {same((int)(uint32_t)a), same((int)(uint32_t)(a >> 32)), same((int)min(bytes, (int64_t)0x7ffffff0)), 0x00020000};
     return r;
 }
 __device__ __forceinline__ void load16_to_lds(i32x4 extent, unsigned lds_wave_base, unsigned offset) {
@@ -59,7 +59,8 @@ struct Operand {
 };
 
 // A tile of W rows and one reduction step in LDS.
-//   along: [W][128 bytes], the 16-byte pieces of a row permuted by the row's low bits (eight rows then hit all banks)
+//   along: [W][128 bytes], the 16-byte pieces of a row permuted by the row's bits 1 to 3: of 16 rows, whose same piece the lanes
+//     of a read ask for together, each then lies in banks of its own (two rows cover them; by bits 0 to 2, rows 8 apart met)
 //   across, bf16: [64 k][W] with the 32-byte pieces of a k permuted by its low bits: a transposing read takes two
 //     neighbouring pieces of four consecutive k, which then fall into different banks
 //   across, float32: [32 k][W] as it is
@@ -71,17 +72,22 @@ template <typename T, bool ALONG, int W, int THREADS> struct Tile {
 
     unsigned offset[LOADS];      // this lane's, from the step's start
     unsigned piece_at;           // along: where in the step this lane's pieces lie (the same for all its loads)
+    // of the step that is loaded next: where it starts, bytes of the operand from there on, bytes of a row's reduction
+    const char* next;
+    int64_t left, stride;
+    int row_left;
 
     __device__ __forceinline__ static int swizzle(int k) { return W >= 128 ? (k & 3) << 1 : k & 3; }
 
     __device__ __forceinline__ void init(const Operand& o, int64_t first_row, int row_bytes) {
+        stride = ALONG ? kStepBytes : STEP * o.ld;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int slot = i * THREADS + (int)threadIdx.x, line = slot / PIECES, s = slot % PIECES;
             if (ALONG) {
-                const int piece = s ^ (line & 7);
+                const int piece = s ^ ((line >> 1) & 7);
                 offset[i] = (unsigned)(line * o.ld) + piece * 16;
-                if (i == 0) piece_at = piece * 16;         // (THREADS / 8 lines further on the low bits are the same)
+                if (i == 0) piece_at = piece * 16;         // (THREADS / 8 lines further on those bits are the same)
             } else {
                 const int piece = ESZ == 2 ? ((((s >> 1) ^ swizzle(line)) << 1) | (s & 1)) : s;
                 const bool there = first_row * ESZ + piece * 16 < row_bytes;
@@ -89,23 +95,32 @@ template <typename T, bool ALONG, int W, int THREADS> struct Tile {
             }
         }
     }
-    // k: elements of the reduction from the step's first on; base: where that step starts
-    __device__ __forceinline__ void load(const Operand& o, const char* base, int64_t first_row, int row_bytes, int64_t k, unsigned lds) {
-        const i32x4 e = extent_of(base, ALONG ? (o.rows - first_row - 1) * o.ld + k * ESZ : (k - 1) * o.ld + row_bytes - first_row * ESZ);
+    // from step s on, of `k` elements of the reduction in all; plane: bytes to the operand's plane
+    __device__ __forceinline__ void start(const Operand& o, int64_t plane, int64_t first_row, int row_bytes, int64_t k, int64_t s) {
+        k -= s * STEP;
+        next = o.p + plane + (ALONG ? first_row * o.ld : first_row * ESZ) + s * stride;
+        left = ALONG ? (o.rows - first_row - 1) * o.ld + k * ESZ : (k - 1) * o.ld + row_bytes - first_row * ESZ;
+        row_left = (int)min(k * ESZ, (int64_t)0x7ffffff0);
+    }
+    __device__ __forceinline__ void load(unsigned lds) {
+        const i32x4 e = extent_of(next, left);
         const unsigned wave = (unsigned)__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * 1024;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             unsigned at = offset[i];
-            if (ALONG && k < STEP) at = piece_at < (unsigned)(k * ESZ) ? at : kNowhere;
+            if (ALONG) at = (int)piece_at < row_left ? at : kNowhere;
             load16_to_lds(e, lds + wave + i * THREADS * 16, at);
         }
+        next += stride;
+        left -= stride;
+        if (ALONG) row_left -= kStepBytes;
     }
     // Fragment of rows [r32, r32 + 32) for the g-th eighth of 16 bytes x 2 of the step: a lane has row r32 + lane % 32 and
     // the half of the group's reduction that lane / 32 names (bf16: 8 elements, float32: 4, each for one of 4 instructions)
     __device__ __forceinline__ static uint4 fragment(const char* tile, int r32, int g, int lane) {
         if constexpr (ALONG) {
             const int r = r32 + (lane & 31);
-            return *reinterpret_cast<const uint4*>(tile + r * kStepBytes + (((2 * g + (lane >> 5)) ^ (r & 7)) << 4));
+            return *reinterpret_cast<const uint4*>(tile + r * kStepBytes + (((2 * g + (lane >> 5)) ^ ((r >> 1) & 7)) << 4));
         } else if constexpr (ESZ == 2) {
             // the transposing read hands lane l of 16 lanes element l of the 16 channels of a piece, for four consecutive k
             // whose lines lanes 4q .. 4q + 3 address, eight bytes each
@@ -229,15 +244,19 @@ __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmAr
     ta.init(g.a, m0, g.a_row_bytes);
     tb.init(g.b, n0, g.b_row_bytes);
     const int first = cut * g.steps_per_cut, last = min(first + g.steps_per_cut, g.steps), steps = last - first, all = steps * g.planes;
-    const char* const a0 = g.a.p + (A_ALONG ? m0 * g.a.ld : m0 * TA::ESZ);
-    const char* const b0 = g.b.p + (B_ALONG ? n0 * g.b.ld : n0 * TB::ESZ);
-    const int64_t a_step = A_ALONG ? kStepBytes : STEP * g.a.ld, b_step = B_ALONG ? kStepBytes : STEP * g.b.ld;
-    int at = 0, plane = 0;                                  // the step that is loaded next
+    int at = steps, plane = 0;                              // steps of this plane that are still to be loaded
+    ta.start(g.a, 0, m0, g.a_row_bytes, g.a_k, first);
+    tb.start(g.b, 0, n0, g.b_row_bytes, g.b_k, first);
     auto load = [&](int stage) {
-        const int64_t s = first + at;
-        ta.load(g.a, a0 + plane * g.a_plane + s * a_step, m0, g.a_row_bytes, g.a_k - s * STEP, lds + stage * STAGE);
-        tb.load(g.b, b0 + s * b_step, n0, g.b_row_bytes, g.b_k - s * STEP, lds + stage * STAGE + TA::BYTES);
-        if (++at == steps) { at = 0; ++plane; }
+        if (at == 0) {
+            at = steps;
+            ++plane;
+            ta.start(g.a, plane * g.a_plane, m0, g.a_row_bytes, g.a_k, first);
+            tb.start(g.b, 0, n0, g.b_row_bytes, g.b_k, first);
+        }
+        --at;
+        ta.load(lds + stage * STAGE);
+        tb.load(lds + stage * STAGE + TA::BYTES);
     };
     floatx16 acc[TM][TN];
 #pragma unroll
@@ -248,27 +267,35 @@ __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmAr
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
     float a_sum[TM] = {};
     const bool sum_a = WANT == PRODUCT && g.dbias != nullptr && tn == 0 && wn == 0;
-    // two stages of LDS: while one is contracted the loads of the next are in flight; fragments are read one group of
-    // instructions ahead (the barriers keep the compiler from moving them back)
+    // Two stages of LDS.  Fragments are read one group of instructions ahead, the first ones of the next step before the last
+    // group of this one: by then all waves have read the rest of this step, so the barrier that says the next step is there also
+    // frees this one's stage for the step after it.  (The scheduling barriers keep the compiler from moving the reads back.)
     auto contract_all = [&](auto with_sum) {
-        if (all > 0) load(0);
+        if (all <= 0) return;
+        uint4 fa[2][TM], fb[2][TN];
+        auto read = [&](int stage, int q) {
+            const char* const A = smem + stage * STAGE;
+#pragma unroll
+            for (int i = 0; i < TM; ++i) fa[q & 1][i] = TA::fragment(A, (wm * TM + i) * 32, q, lane);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) fb[q & 1][j] = TB::fragment(A + TA::BYTES, (wn * TN + j) * 32, q, lane);
+        };
+        load(0);
+        wait_loads<0>();
+        __syncthreads();
+        if (all > 1) load(1);
+        read(0, 0);
         for (int t = 0; t < all; ++t) {
-            wait_loads<0>();
-            __syncthreads();           // this step is there for all waves, and all are done with the stage that is filled now
-            const char* const A = smem + (t & 1) * STAGE;
-            const char* const B = A + TA::BYTES;
-            uint4 fa[2][TM], fb[2][TN];
-            auto read = [&](int q) {
-#pragma unroll
-                for (int i = 0; i < TM; ++i) fa[q & 1][i] = TA::fragment(A, (wm * TM + i) * 32, q, lane);
-#pragma unroll
-                for (int j = 0; j < TN; ++j) fb[q & 1][j] = TB::fragment(B, (wn * TN + j) * 32, q, lane);
-            };
-            read(0);
-            if (t + 1 < all) load((t + 1) & 1);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                if (q < 3) read(q + 1);
+                if (q < 3) {
+                    read(t & 1, q + 1);
+                } else if (t + 1 < all) {
+                    wait_loads<0>();
+                    __syncthreads();
+                    if (t + 2 < all) load(t & 1);
+                    read((t + 1) & 1, 0);
+                }
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                 for (int i = 0; i < TM; ++i)
@@ -281,6 +308,7 @@ __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmAr
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
+        __syncthreads();           // LDS is free
     };
     if (WANT == PRODUCT && sum_a) contract_all(std::true_type{});
     else contract_all(std::false_type{});
