@@ -5,16 +5,19 @@
 //   lse, entropy, log_prob              from each tile's sums (softmax_sums.h), joined over the tiles of a row
 //   dz = g (1[c = t] - p) - h p (log p + H),  dx = dz w,  dw = dz^T x,  db = sum of dz over the rows
 //
-// Four products, one kernel (gemm_kernel) on 32x32 matrix instructions.  An operand lies with the reduction along its rows
-// (x and w in z, dz in dx) or across them (dz and x in dw, w in dx); either is brought to LDS as it lies, and a fragment of
-// the second kind is read transposed, so nothing is transposed in memory.  z is formed as w x^T: a lane then has one row's
-// classes, 16 to a 32x32 tile, and the sums over classes stay inside it.
+// Four products, one kernel (gemm_kernel) on 32x32 bf16 matrix instructions.  An operand lies with the reduction along its
+// rows (x and w in z, dz in dx) or across them (dz and x in dw, w in dx); either is brought to LDS as it lies, and a fragment
+// of the second kind is read transposed, so nothing is transposed in memory.  z is formed as w x^T: a lane then has one
+// row's classes, 16 to a 32x32 tile, and the sums over classes stay inside it.
+//
+// Float32 operands are sums of three bf16 numbers ("planes", 24 bits together), and a product of two such sums is the six
+// products of planes that are not below float32's last place.  The matrix cores do 16 bf16 multiplications in the time of one float32 one,
+// so six of them still take less than half of its time.
 //
 // The gradient forms z again rather than keep it, a piece of the classes at a time.  dz is stored for the two products that
-// read it: in float32 as it is, in bf16 as a sum of three bf16 numbers (24 bits), because dw is float32 and a single
-// rounding of dz would be its largest error by four orders of magnitude; dx, which is rounded to bf16, takes the first two.
+// read it, in both types as three planes: dw is float32, and a single rounding of dz to bf16 would be its largest error by
+// four orders of magnitude.  dx of bf16, which is rounded to bf16 itself, takes the first two.
 #include <algorithm>
-#include <type_traits>
 
 #include "operators.h"
 #include "profiler.h"
@@ -30,9 +33,6 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 
-constexpr int kStepBytes = 128;        // of a reduction step along a row
-constexpr int kTile = 128, kBigTile = 256;     // rows and columns of a block's tile
-
 // ---- operands ---------------------------------------------------------------------------------------------------------
 // 16 bytes per lane from memory to LDS: lane l's go to lds_wave_base + 16 l; lanes whose offset lies past the descriptor's
 // extent get zeros.  Issued from assembly, so that the compiler does not wait for it at every LDS access: wait_loads and a
@@ -41,7 +41,7 @@ constexpr unsigned kNowhere = 0x80000000u;       // past any extent (they are cl
 __device__ __forceinline__ i32x4 extent_of(const char* p, int64_t bytes) {
     const uint64_t a = (uint64_t)p;
     auto same = [](int v) { return __builtin_amdgcn_readfirstlane(v); };       // (they are: the compiler has lost track)
-    const i32x4 r = {same((int)(uint32_t)a), same((int)(uint32_t)(a >> 32)), same((int)min(bytes, (int64_t)0x7ffffff0)), 0x00020000};
+    const i32x4 r = {same((int)(uint32_t)a), same((int)(uint32_t)(a >> 32)), same((int)max((int64_t)0, min(bytes, (int64_t)0x7ffffff0))), 0x00020000};
     return r;
 }
 __device__ __forceinline__ void load16_to_lds(i32x4 extent, unsigned lds_wave_base, unsigned offset) {
@@ -49,90 +49,90 @@ __device__ __forceinline__ void load16_to_lds(i32x4 extent, unsigned lds_wave_ba
 }
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
-// One operand of a product: `rows` of it matter, `k` elements of the reduction.  along: row r's reduction lies at
-// p + r * ld; otherwise element (r, k) is at p + k * ld + r.  Bytes; p, ld and the bytes of a row are multiples of 16
-// and hold zeros past the operand's elements.
+// One operand of a product: element (r, k) of `rows` by `k` of the reduction, bf16.  along: row r's reduction lies at
+// p + r * ld; across: k's rows lie at p + k * ld.  A line's elements follow each other, or, of an operand of three planes, in
+// groups of 16: the group's first plane, second, third (32 bytes each).  p and ld are multiples of 16 bytes, a line's elements
+// whole pieces of 8 (of planes: groups of 16) with zeros past the operand's.
 struct Operand {
     const char* p;
-    int64_t ld;
-    int64_t rows;
+    int64_t ld;                // bytes
+    int64_t rows, k;
+    int stored;                // planes in memory: 1 or 3
+    __host__ __device__ int64_t line_bytes(int64_t n) const { return stored == 1 ? (n + 7) / 8 * 16 : (n + 15) / 16 * 32 * stored; }
 };
 
-// A tile of W rows and one reduction step in LDS.
-//   along: [W][128 bytes], the 16-byte pieces of a row permuted by the row's bits 1 to 3: of 16 rows, whose same piece the lanes
-//     of a read ask for together, each then lies in banks of its own (two rows cover them; by bits 0 to 2, rows 8 apart met)
-//   across, bf16: [64 k][W] with the 32-byte pieces of a k permuted by its low bits: a transposing read takes two
-//     neighbouring pieces of four consecutive k, which then fall into different banks
-//   across, float32: [32 k][W] as it is
-template <typename T, bool ALONG, int W, int THREADS> struct Tile {
-    static constexpr int ESZ = (int)sizeof(T), STEP = kStepBytes / ESZ, BYTES = W * kStepBytes;
-    static constexpr int PIECES = ALONG ? 8 : W * ESZ / 16;            // 16-byte pieces of a line
+// Tiles of W rows and one reduction step of KS elements in LDS, one for each of the first P planes.
+//   along: [W][KS], the 16-byte pieces of a row permuted by bits of the row's number, such that the 16 rows whose same piece the
+//     lanes of a read ask for together lie in banks of their own
+//   across: [KS][W], the 32-byte pairs of pieces of a k permuted by its low bits: a transposing read takes two neighbouring
+//     pairs of four consecutive k, which then fall into different banks
+template <bool ALONG, int W, int P, int KS, int THREADS> struct Tile {
+    static constexpr int PLANE = W * KS * 2, BYTES = P * PLANE;
+    static constexpr int PIECES = ALONG ? KS / 8 : W / 8;              // 16-byte pieces of a line
     static constexpr int LOADS = BYTES / 16 / THREADS;                 // per lane
     static_assert(BYTES % (16 * THREADS) == 0, "whole loads");
+    static_assert(!ALONG || THREADS % (16 * PIECES) == 0, "a lane's loads are of the same piece of their rows");
 
     unsigned offset[LOADS];      // this lane's, from the step's start
-    unsigned piece_at;           // along: where in the step this lane's pieces lie (the same for all its loads)
-    // of the step that is loaded next: where it starts, bytes of the operand from there on, bytes of a row's reduction
+    int piece_k;                 // along: which of the step's elements this lane's pieces hold first
+    // of the step that is loaded next: where it starts, bytes of the operand from there on, elements of the reduction
     const char* next;
     int64_t left, stride;
-    int row_left;
+    int k_left;
+    // of the step that is being loaded
+    i32x4 extent;
+    int k_here;
 
-    __device__ __forceinline__ static int swizzle(int k) { return W >= 128 ? (k & 3) << 1 : k & 3; }
+    __device__ __forceinline__ static int pair_of(int pair, int k) { return pair ^ ((k & 3) << 1); }
+    __device__ __forceinline__ static int piece_of(int piece, int row) { return piece ^ ((row * PIECES / 16) & (PIECES - 1)); }
 
-    __device__ __forceinline__ void init(const Operand& o, int64_t first_row, int row_bytes) {
-        stride = ALONG ? kStepBytes : STEP * o.ld;
+    __device__ __forceinline__ void init(const Operand& o, int64_t first_row) {
+        stride = ALONG ? (int64_t)KS * 2 * o.stored : KS * o.ld;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int slot = i * THREADS + (int)threadIdx.x, line = slot / PIECES, s = slot % PIECES;
-            if (ALONG) {
-                const int piece = s ^ ((line >> 1) & 7);
-                offset[i] = (unsigned)(line * o.ld) + piece * 16;
-                if (i == 0) piece_at = piece * 16;         // (THREADS / 8 lines further on those bits are the same)
-            } else {
-                const int piece = ESZ == 2 ? ((((s >> 1) ^ swizzle(line)) << 1) | (s & 1)) : s;
-                const bool there = first_row * ESZ + piece * 16 < row_bytes;
-                offset[i] = there ? (unsigned)(line * o.ld) + piece * 16 : kNowhere;
-            }
+            const int slot = i * THREADS + (int)threadIdx.x, plane = slot / (PLANE / 16), line = slot % (PLANE / 16) / PIECES, s = slot % PIECES;
+            const int piece = ALONG ? piece_of(s, line) : pair_of(s >> 1, line) << 1 | (s & 1);
+            const unsigned at = (unsigned)(line * o.ld) + ((piece >> 1) * o.stored + plane) * 32 + (piece & 1) * 16;
+            offset[i] = ALONG || first_row + piece * 8 < o.rows ? at : kNowhere;
+            if (ALONG && i == 0) piece_k = piece * 8;
         }
     }
-    // from step s on, of `k` elements of the reduction in all; plane: bytes to the operand's plane
-    __device__ __forceinline__ void start(const Operand& o, int64_t plane, int64_t first_row, int row_bytes, int64_t k, int64_t s) {
-        k -= s * STEP;
-        next = o.p + plane + (ALONG ? first_row * o.ld : first_row * ESZ) + s * stride;
-        left = ALONG ? (o.rows - first_row - 1) * o.ld + k * ESZ : (k - 1) * o.ld + row_bytes - first_row * ESZ;
-        row_left = (int)min(k * ESZ, (int64_t)0x7ffffff0);
+    __device__ __forceinline__ void start(const Operand& o, int64_t first_row, int64_t step) {
+        next = o.p + (ALONG ? first_row * o.ld : first_row * 2 * o.stored) + step * stride;
+        left = ALONG ? (o.rows - first_row - 1) * o.ld + o.line_bytes(o.k) - step * stride
+                     : (o.k - step * KS - 1) * o.ld + o.line_bytes(o.rows) - first_row * 2 * o.stored;
+        k_left = (int)min(o.k - step * KS, (int64_t)0x7fffffff);
     }
-    __device__ __forceinline__ void load(unsigned lds) {
-        const i32x4 e = extent_of(next, left);
-        const unsigned wave = (unsigned)__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * 1024;
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            unsigned at = offset[i];
-            if (ALONG) at = (int)piece_at < row_left ? at : kNowhere;
-            load16_to_lds(e, lds + wave + i * THREADS * 16, at);
-        }
+    // Turns to the next step; there: false past the last one (its loads bring zeros into a stage that nobody reads, so that
+    // loads can be counted).
+    __device__ __forceinline__ void turn(bool there) {
+        extent = extent_of(next, there ? left : 0);
+        k_here = k_left;
         next += stride;
         left -= stride;
-        if (ALONG) row_left -= kStepBytes;
+        k_left -= KS;
     }
-    // Fragment of rows [r32, r32 + 32) for the g-th eighth of 16 bytes x 2 of the step: a lane has row r32 + lane % 32 and
-    // the half of the group's reduction that lane / 32 names (bf16: 8 elements, float32: 4, each for one of 4 instructions)
-    __device__ __forceinline__ static uint4 fragment(const char* tile, int r32, int g, int lane) {
+    // the i-th of this step's loads
+    __device__ __forceinline__ void load(int i, unsigned lds) const {
+        const unsigned wave = (unsigned)__builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * 1024;
+        load16_to_lds(extent, lds + wave + i * THREADS * 16, !ALONG || piece_k < k_here ? offset[i] : kNowhere);
+    }
+    // Fragment of rows [r32, r32 + 32) and reduction elements [16 q, 16 q + 16) of the step: a lane has row r32 + lane % 32 and
+    // the eight elements of half lane / 32
+    __device__ __forceinline__ static uint4 fragment(const char* tile, int plane, int r32, int q, int lane) {
+        tile += plane * PLANE;
         if constexpr (ALONG) {
             const int r = r32 + (lane & 31);
-            return *reinterpret_cast<const uint4*>(tile + r * kStepBytes + (((2 * g + (lane >> 5)) ^ ((r >> 1) & 7)) << 4));
-        } else if constexpr (ESZ == 2) {
-            // the transposing read hands lane l of 16 lanes element l of the 16 channels of a piece, for four consecutive k
-            // whose lines lanes 4q .. 4q + 3 address, eight bytes each
+            return *reinterpret_cast<const uint4*>(tile + r * KS * 2 + piece_of(2 * q + (lane >> 5), r) * 16);
+        } else {
+            // the transposing read hands lane l of 16 lanes element l of the 16 rows of a pair, for four consecutive k whose
+            // lines lanes 4i .. 4i + 3 address, eight bytes each
             typedef shortx4 __attribute__((address_space(3))) * lds_ptr;
-            const int ch = r32 + ((lane >> 4) & 1) * 16 + 4 * (lane & 3), k = g * 16 + (lane >> 5) * 8 + ((lane & 15) >> 2);
-            auto at = [&](int kk) { return (lds_ptr)(tile + (kk * W + ((((ch >> 4) ^ swizzle(kk)) << 4) | (ch & 15))) * 2); };
+            const int row = r32 + ((lane >> 4) & 1) * 16 + 4 * (lane & 3), k = q * 16 + (lane >> 5) * 8 + ((lane & 15) >> 2);
+            auto at = [&](int kk) { return (lds_ptr)(tile + kk * W * 2 + pair_of(row >> 4, kk) * 32 + (row & 15) * 2); };
             const uint2 a = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(at(k)));
             const uint2 b = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(at(k + 4)));
             return make_uint4(a.x, a.y, b.x, b.y);
-        } else {
-            const uint32_t* q = reinterpret_cast<const uint32_t*>(tile) + (g * 8 + (lane >> 5) * 4) * W + r32 + (lane & 31);
-            return make_uint4(q[0], q[W], q[2 * W], q[3 * W]);
         }
     }
 };
@@ -147,15 +147,6 @@ template <typename T> __device__ __forceinline__ void multiply(const uint4& a, c
         c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.w), __uint_as_float(b.w), c, 0, 0, 0);
     }
 }
-// sum of a fragment's elements of this lane
-template <typename T> __device__ __forceinline__ float fragment_sum(const uint4& f) {
-    Vec16<T> v;
-    v.u = f;
-    float s = 0.f;
-#pragma unroll
-    for (int e = 0; e < Elem<T>::VEC; ++e) s += Elem<T>::to_f32(v.e[e]);
-    return s;
-}
 // row of a 32x32 tile that element e of a lane's 16 stands for (its column is lane % 32)
 __device__ __forceinline__ int tile_row(int e, int lane) { return 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3); }
 
@@ -168,26 +159,17 @@ __device__ __forceinline__ uint2 next_bf16(float (&v)[4]) {
     v[3] -= __uint_as_float(b.y & 0xffff0000u);
     return b;
 }
-
-// four neighbouring classes of a row of dz
-template <typename T> __device__ __forceinline__ void store_dz(char* p, int64_t plane, const float (&d)[4]) {
-    if constexpr (sizeof(T) == 4) {
-        *reinterpret_cast<float4*>(p) = make_float4(d[0], d[1], d[2], d[3]);
-    } else {
-        float v[4] = {d[0], d[1], d[2], d[3]};
+// four neighbouring elements, the first of them number c (a multiple of 4), of a line of three planes
+__device__ __forceinline__ void store_planes(char* line, int64_t c, float (&v)[4]) {
+    char* const p = line + (c >> 4) * 96 + (c & 15) * 2;
 #pragma unroll
-        for (int q = 0; q < 3; ++q) *reinterpret_cast<uint2*>(p + q * plane) = next_bf16(v);
-    }
+    for (int q = 0; q < 3; ++q) *reinterpret_cast<uint2*>(p + q * 32) = next_bf16(v);
 }
 
 enum Want { SUMS, GRADS, PRODUCT };     // of z: sums over classes, dz; of the others: the product itself
 
 struct GemmArgs {
     Operand a, b;
-    int64_t a_k, b_k;          // elements of the reduction that lie there (an operand along it has them up to whole 16 bytes)
-    int64_t a_plane;           // bytes between the numbers that a's elements are the sum of
-    int planes;
-    int a_row_bytes, b_row_bytes;      // of an operand that lies across
     int steps, steps_per_cut;  // of the reduction; a cut of it is a block's
     int tiles_m, tiles_n, group;
     // z: a = w from class `first_class` on, b = x
@@ -196,14 +178,14 @@ struct GemmArgs {
     RowFacts facts;
     float4* sums;              // [tile of classes][rows]: m, s, t
     float* target_z;
-    char* dz;                  // [planes][rows][dz_ld], of the classes from first_class on
-    int64_t dz_ld, dz_plane;   // bytes
-    int dz_classes;            // columns of dz that are written (zeros past the last class)
+    char* dz;                  // [rows][dz_ld bytes] of the classes from first_class on, three planes
+    int64_t dz_ld;
+    int dz_classes;            // of whole groups (zeros past the last class)
+    float* db;                 // [tile of rows][db_ld] sums of dz; null: not wanted
+    int64_t db_ld;
     // products
     void* out;                 // [cut][a.rows][out_ld]
     int64_t out_ld, out_cut;   // elements
-    float* dbias;              // [cut][a.rows] sums of a over the reduction; null: none
-    int64_t dbias_cut;
 };
 
 // (tile of a's rows, of b's rows, cut).  Consecutive blocks go to the eight dies in turn; a die's blocks are made
@@ -223,40 +205,44 @@ __device__ __forceinline__ void tile_of(const GemmArgs& g, int& tm, int& tn, int
 
 // A block's waves, WM x WN, and a wave's 32x32 tiles, TM x TN.  64x64 to a wave read 4 KB of LDS for every 4 matrix
 // instructions, 128x64 read 6 KB for 8; what the larger tile needs is enough of them for the chip.
-struct Shape128 { static constexpr int WM = 2, WN = 2, TM = 2, TN = 2; };
-struct Shape256 { static constexpr int WM = 2, WN = 4, TM = 4, TN = 2; };
+struct Shape128 { static constexpr int WM = 2, WN = 2, TM = 2, TN = 2, SIDE = 128; };
+struct Shape256 { static constexpr int WM = 2, WN = 4, TM = 4, TN = 2, SIDE = 256; };
+// Elements of a reduction step and steps in LDS at a time, for PA and PB planes: 32 KB (256x256 tiles: 64 at most) to a step, and
+// as many as fit, so that loads of the steps to come are always in flight.
+template <int PA, int PB> struct Steps { static constexpr int KS = PA + PB <= 3 ? 32 : 16, STAGES = PA + PB == 2 || PA + PB == 4 ? 4 : 3; };
 
-template <typename T, Want WANT, bool A_ALONG, bool B_ALONG, typename OUT, typename SHAPE>
+template <Want WANT, int PA, int PB, bool A_ALONG, bool B_ALONG, typename OUT, typename SHAPE>
 __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmArgs g) {
-    constexpr int WM = SHAPE::WM, WN = SHAPE::WN, TM = SHAPE::TM, TN = SHAPE::TN, THREADS = WM * WN * 64;
-    constexpr int MT = WM * TM * 32, NT = WN * TN * 32;
-    typedef Tile<T, A_ALONG, MT, THREADS> TA;
-    typedef Tile<T, B_ALONG, NT, THREADS> TB;
-    constexpr int STAGE = TA::BYTES + TB::BYTES, STEP = TA::STEP;
-    __shared__ __attribute__((aligned(16))) char smem[2 * STAGE];
+    constexpr int WM = SHAPE::WM, WN = SHAPE::WN, TM = SHAPE::TM, TN = SHAPE::TN, THREADS = WM * WN * 64, SIDE = SHAPE::SIDE;
+    constexpr int KS = Steps<PA, PB>::KS, STAGES = Steps<PA, PB>::STAGES;
+    typedef Tile<A_ALONG, SIDE, PA, KS, THREADS> TA;
+    typedef Tile<B_ALONG, SIDE, PB, KS, THREADS> TB;
+    constexpr int STAGE = TA::BYTES + TB::BYTES;
+    __shared__ __attribute__((aligned(16))) char smem[STAGES * STAGE];
     const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
     int tm, tn, cut;
     tile_of(g, tm, tn, cut);
-    const int64_t m0 = (int64_t)tm * MT, n0 = (int64_t)tn * NT;
+    const int64_t m0 = (int64_t)tm * SIDE, n0 = (int64_t)tn * SIDE;
+    const int first = cut * g.steps_per_cut, all = min(g.steps_per_cut, g.steps - first);
     TA ta;
     TB tb;
-    ta.init(g.a, m0, g.a_row_bytes);
-    tb.init(g.b, n0, g.b_row_bytes);
-    const int first = cut * g.steps_per_cut, last = min(first + g.steps_per_cut, g.steps), steps = last - first, all = steps * g.planes;
-    int at = steps, plane = 0;                              // steps of this plane that are still to be loaded
-    ta.start(g.a, 0, m0, g.a_row_bytes, g.a_k, first);
-    tb.start(g.b, 0, n0, g.b_row_bytes, g.b_k, first);
-    auto load = [&](int stage) {
-        if (at == 0) {
-            at = steps;
-            ++plane;
-            ta.start(g.a, plane * g.a_plane, m0, g.a_row_bytes, g.a_k, first);
-            tb.start(g.b, 0, n0, g.b_row_bytes, g.b_k, first);
-        }
-        --at;
-        ta.load(lds + stage * STAGE);
-        tb.load(lds + stage * STAGE + TA::BYTES);
+    ta.init(g.a, m0);
+    tb.init(g.b, n0);
+    ta.start(g.a, m0, first);
+    tb.start(g.b, n0, first);
+    int asked = 0, to = 0;                                  // steps asked for, and the stage of the one being loaded
+    auto turn = [&]() {
+        const bool there = asked < all;
+        ta.turn(there);
+        tb.turn(there);
+        if (asked > 0) to = to + 1 == STAGES ? 0 : to + 1;
+        ++asked;
+    };
+    constexpr int LOADS = TA::LOADS + TB::LOADS, GROUPS = KS / 16 * PA;
+    auto load = [&](int i) {
+        if (i < TA::LOADS) ta.load(i, lds + to * STAGE);
+        else tb.load(i - TA::LOADS, lds + to * STAGE + TA::BYTES);
     };
     floatx16 acc[TM][TN];
 #pragma unroll
@@ -265,53 +251,48 @@ __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmAr
         for (int j = 0; j < TN; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
-    float a_sum[TM] = {};
-    const bool sum_a = WANT == PRODUCT && g.dbias != nullptr && tn == 0 && wn == 0;
-    // Two stages of LDS.  Fragments are read one group of instructions ahead, the first ones of the next step before the last
-    // group of this one: by then all waves have read the rest of this step, so the barrier that says the next step is there also
-    // frees this one's stage for the step after it.  (The scheduling barriers keep the compiler from moving the reads back.)
-    auto contract_all = [&](auto with_sum) {
-        if (all <= 0) return;
-        uint4 fa[2][TM], fb[2][TN];
-        auto read = [&](int stage, int q) {
-            const char* const A = smem + stage * STAGE;
 #pragma unroll
-            for (int i = 0; i < TM; ++i) fa[q & 1][i] = TA::fragment(A, (wm * TM + i) * 32, q, lane);
+    for (int u = 0; u < STAGES - 1; ++u) {
+        turn();
 #pragma unroll
-            for (int j = 0; j < TN; ++j) fb[q & 1][j] = TB::fragment(A + TA::BYTES, (wn * TN + j) * 32, q, lane);
-        };
-        load(0);
-        wait_loads<0>();
+        for (int i = 0; i < LOADS; ++i) load(i);
+    }
+    for (int t = 0, from = 0; t < all; ++t, from = from + 1 == STAGES ? 0 : from + 1) {
+        // This step is there for all waves, and all are done with the one before, whose stage is filled now.  (Loads come in
+        // order: all but those of the STAGES - 2 younger steps have.)  A wave asks for its part of a step between its groups of
+        // matrix instructions: the path to memory takes a load every 16 cycles, and if all waves ask at once the matrix cores
+        // wait for that.
+        wait_loads<(STAGES - 2) * LOADS>();
         __syncthreads();
-        if (all > 1) load(1);
-        read(0, 0);
-        for (int t = 0; t < all; ++t) {
+        turn();
+        const char* const A = smem + from * STAGE;
+        const char* const B = A + TA::BYTES;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                if (q < 3) {
-                    read(t & 1, q + 1);
-                } else if (t + 1 < all) {
-                    wait_loads<0>();
-                    __syncthreads();
-                    if (t + 2 < all) load(t & 1);
-                    read((t + 1) & 1, 0);
-                }
-                __builtin_amdgcn_sched_barrier(0);
+        for (int q = 0; q < KS / 16; ++q) {
+            uint4 fb[PB][TN];
 #pragma unroll
-                for (int i = 0; i < TM; ++i)
+            for (int b = 0; b < PB; ++b)
 #pragma unroll
-                    for (int j = 0; j < TN; ++j) multiply<T>(fa[q & 1][i], fb[q & 1][j], acc[i][j]);
-                if constexpr (decltype(with_sum)::value) {
+                for (int j = 0; j < TN; ++j) fb[b][j] = TB::fragment(B, b, (wn * TN + j) * 32, q, lane);
 #pragma unroll
-                    for (int i = 0; i < TM; ++i) a_sum[i] += fragment_sum<T>(fa[q & 1][i]);
-                }
-                __builtin_amdgcn_sched_barrier(0);
+            for (int a = 0; a < PA; ++a) {
+                uint4 fa[TM];
+#pragma unroll
+                for (int i = 0; i < TM; ++i) fa[i] = TA::fragment(A, a, (wm * TM + i) * 32, q, lane);
+#pragma unroll
+                for (int b = 0; b < PB && a + b < (PA > PB ? PA : PB); ++b)
+#pragma unroll
+                    for (int i = 0; i < TM; ++i)
+#pragma unroll
+                        for (int j = 0; j < TN; ++j) multiply<bf16_t>(fa[i], fb[b][j], acc[i][j]);
+                const int group = q * PA + a;
+#pragma unroll
+                for (int i = group * LOADS / GROUPS; i < (group + 1) * LOADS / GROUPS; ++i) load(i);
             }
         }
-        __syncthreads();           // LDS is free
-    };
-    if (WANT == PRODUCT && sum_a) contract_all(std::true_type{});
-    else contract_all(std::false_type{});
+    }
+    wait_loads<0>();
+    __syncthreads();           // LDS is free
     if constexpr (WANT == PRODUCT) {
         OUT* const out = (OUT*)g.out + cut * g.out_cut;
 #pragma unroll
@@ -326,17 +307,9 @@ __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmAr
                     if (m < g.a.rows) out[m * g.out_ld + n] = Elem<OUT>::from_f32(acc[i][j][e]);
                 }
         }
-        if (sum_a) {
-#pragma unroll
-            for (int i = 0; i < TM; ++i) {
-                const float s = a_sum[i] + __shfl_xor(a_sum[i], 32, 64);
-                const int64_t m = m0 + (wm * TM + i) * 32 + (lane & 31);
-                if (lane < 32 && m < g.a.rows) g.dbias[cut * g.dbias_cut + m] = s;
-            }
-        }
     } else {
-        // z: rows of the tile are classes, columns rows of x
-        // class of element e of tile i: c0 + 32 i + 8 (e / 4) + e % 4; those from c0 + left on are none
+        // z: rows of the tile are classes, columns rows of x.  Class of element e of tile i: c0 + place(i, e); those from c0 + left
+        // on are none
         const int64_t c0 = g.first_class + m0 + wm * TM * 32 + 4 * (lane >> 5);
         const int left = (int)min((int64_t)4096, g.classes - c0);
         auto place = [](int i, int e) { return 32 * i + 8 * (e >> 2) + (e & 3); };
@@ -346,8 +319,7 @@ __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmAr
 #pragma unroll
             for (int e = 0; e < 16; ++e) bias[i][e] = g.bias != nullptr && place(i, e) < left ? g.bias[c0 + place(i, e)] : 0.f;
         if constexpr (WANT == SUMS) {
-            __syncthreads();                   // LDS is the sums' now
-            float4* const part = reinterpret_cast<float4*>(smem);      // [wm][NT]
+            float4* const part = reinterpret_cast<float4*>(smem);      // [wm][SIDE]
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
                 const int col = (wn * TN + j) * 32 + (lane & 31);
@@ -372,15 +344,15 @@ __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmAr
 #pragma unroll
                     for (int e = 0; e < 16; ++e) softmax_add(s, acc[i][j][e], base);
                 softmax_join(s, softmax_shuffle(s, 32));
-                if (lane < 32) part[wm * NT + col] = make_float4(s.m, s.s, s.t, 0.f);
+                if (lane < 32) part[wm * SIDE + col] = make_float4(s.m, s.s, s.t, 0.f);
                 if (here) g.target_z[n] = zt;
             }
             __syncthreads();
-            if (threadIdx.x < NT && n0 + threadIdx.x < g.b.rows) {
+            if (threadIdx.x < SIDE && n0 + threadIdx.x < g.b.rows) {
                 SoftmaxSums s;
 #pragma unroll
                 for (int w = 0; w < WM; ++w) {
-                    const float4 p = part[w * NT + threadIdx.x];
+                    const float4 p = part[w * SIDE + threadIdx.x];
                     SoftmaxSums o;
                     o.m = p.x; o.s = p.y; o.t = p.z;
                     softmax_join(s, o);
@@ -388,10 +360,11 @@ __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmAr
                 g.sums[tm * g.b.rows + n0 + threadIdx.x] = make_float4(s.m, s.s, s.t, 0.f);
             }
         } else {
-            // dz goes out through LDS, a plane at a time, so that rows are written in whole lines: [NT rows][MT classes] with the
-            // 16-byte pieces of a row permuted by its low bits (32 lanes write one piece of 32 rows)
-            constexpr int PLANES = sizeof(T) == 2 ? 3 : 1, PIECES = MT * (int)sizeof(T) / 16;
-            static_assert(NT * MT * (int)sizeof(T) <= 2 * STAGE, "a plane fits");
+            // dz goes out through LDS, a plane at a time, so that rows are written in whole pieces: [SIDE rows][SIDE classes] with
+            // the 16-byte pieces of a row permuted by its low bits (32 lanes write one piece of 32 rows).  A thread moves the same
+            // classes of every (THREADS / PIECES)-th row, whose sum is its part of the bias's gradient.
+            constexpr int PIECES = SIDE / 8, ROWS = THREADS / PIECES;
+            static_assert(SIDE * SIDE * 2 <= STAGES * STAGE && ROWS * SIDE * 4 <= STAGES * STAGE, "fits");
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
                 const int64_t n = n0 + (wn * TN + j) * 32 + (lane & 31);
@@ -402,38 +375,50 @@ __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmAr
 #pragma unroll
                     for (int e = 0; e < 16; ++e) acc[i][j][e] = place(i, e) < left ? row.of(acc[i][j][e] + bias[i][e], place(i, e) == hot) : 0.f;
             }
-            const int wide = (int)min((int64_t)MT, g.dz_classes - m0) * (int)sizeof(T) / 16;       // pieces of a row that are written
+            const int c = threadIdx.x % PIECES, rows = (int)min((int64_t)SIDE, g.b.rows - n0);
+            const bool wanted = m0 + c * 8 < g.dz_classes;
+            float total[8] = {};
 #pragma unroll
-            for (int p = 0; p < PLANES; ++p) {
-                __syncthreads();           // LDS is free: of the product's tiles, then of the plane before
+            for (int p = 0; p < 3; ++p) {
+                if (p > 0) __syncthreads();        // the plane before is out
 #pragma unroll
                 for (int j = 0; j < TN; ++j) {
                     const int r = (wn * TN + j) * 32 + (lane & 31);
-                    char* const line = smem + r * (MT * (int)sizeof(T));
 #pragma unroll
                     for (int i = 0; i < TM; ++i)
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
-                            const int byte = ((wm * TM + i) * 32 + 8 * q + 4 * (lane >> 5)) * (int)sizeof(T);
-                            char* const to = line + (((byte >> 4) ^ (r & (PIECES - 1))) << 4) + (byte & 15);
+                            const int piece = (wm * TM + i) * 4 + q;
                             float d[4];
 #pragma unroll
                             for (int e = 0; e < 4; ++e) d[e] = acc[i][j][4 * q + e];
-                            if constexpr (sizeof(T) == 4) {
-                                *reinterpret_cast<float4*>(to) = make_float4(d[0], d[1], d[2], d[3]);
-                            } else {
-                                *reinterpret_cast<uint2*>(to) = next_bf16(d);
+                            *reinterpret_cast<uint2*>(smem + (r * PIECES + (piece ^ (r & (PIECES - 1)))) * 16 + 8 * (lane >> 5)) = next_bf16(d);
 #pragma unroll
-                                for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = d[e];
-                            }
+                            for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = d[e];
                         }
                 }
                 __syncthreads();
-                char* const out = g.dz + p * g.dz_plane + n0 * g.dz_ld + m0 * (int64_t)sizeof(T);
-                for (int s = threadIdx.x; s < NT * PIECES; s += THREADS) {
-                    const int r = s / PIECES, c = s % PIECES;
-                    if (n0 + r < g.b.rows && c < wide)
-                        *reinterpret_cast<uint4*>(out + r * g.dz_ld + c * 16) = *reinterpret_cast<const uint4*>(smem + (r * PIECES + (c ^ (r & (PIECES - 1)))) * 16);
+                if (wanted) {
+                    char* const out = g.dz + n0 * g.dz_ld + (m0 / 16 + c / 2) * 96 + p * 32 + (c & 1) * 16;
+                    for (int r = threadIdx.x / PIECES; r < rows; r += ROWS) {
+                        Vec16<bf16_t> v;
+                        v.u = *reinterpret_cast<const uint4*>(smem + (r * PIECES + (c ^ (r & (PIECES - 1)))) * 16);
+                        *reinterpret_cast<uint4*>(out + r * g.dz_ld) = v.u;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) total[e] += bf16_to_f32(v.e[e]);
+                    }
+                }
+            }
+            if (g.db != nullptr) {
+                __syncthreads();
+                float* const part = reinterpret_cast<float*>(smem);        // [ROWS][SIDE]
+#pragma unroll
+                for (int e = 0; e < 8; ++e) part[threadIdx.x / PIECES * SIDE + c * 8 + e] = total[e];
+                __syncthreads();
+                if (threadIdx.x < SIDE && g.first_class + m0 + threadIdx.x < g.classes) {
+                    float sum = 0.f;
+                    for (int r = 0; r < ROWS; ++r) sum += part[r * SIDE + threadIdx.x];
+                    g.db[tn * g.db_ld + m0 + threadIdx.x] = sum;
                 }
             }
         }
@@ -444,9 +429,11 @@ __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmAr
 // Where z has too few tiles to fill the chip it is formed in 32x32 tiles with the reduction cut as well, over a block's four
 // waves and over blocks, and its float32 parts are stored: [cut][rows][z_ld].  Fragments come straight from memory (L2: a
 // tile is used by few); what that bounds is the latency of the chain of loads, so each wave has eight in flight.
+constexpr int kStepBytes = 128;        // of a reduction step
+struct Matrix { const char* p; int64_t ld, rows; };        // ld in bytes; 16-byte aligned
 struct ThinArgs {
-    Operand w, x;
-    int64_t k;                 // up to whole 16 bytes
+    Matrix w, x;
+    int64_t row_bytes;         // whole 16 bytes
     int steps, steps_per_wave, tiles_m, tiles_n;
     float* z;
     int64_t z_ld;
@@ -460,7 +447,6 @@ template <typename T> __global__ __launch_bounds__(256) void thin_logits_kernel(
     const int tm = (int)(l % (unsigned)g.tiles_m), cut = (int)(l / (unsigned)g.tiles_m);
     const int64_t m = min((int64_t)tm * 32 + (lane & 31), g.w.rows - 1), n = min((int64_t)tn * 32 + (lane & 31), g.x.rows - 1);
     const int first = (cut * 4 + wave) * g.steps_per_wave, last = min(first + g.steps_per_wave, g.steps);
-    const int64_t end = g.k * (int64_t)sizeof(T);
     int64_t at = (int64_t)first * kStepBytes + 16 * (lane >> 5);
     const char* const a = g.w.p + m * g.w.ld;
     const char* const b = g.x.p + n * g.x.ld;
@@ -471,7 +457,7 @@ template <typename T> __global__ __launch_bounds__(256) void thin_logits_kernel(
         uint4 fa[4], fb[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const bool in = at + 32 * q < end;
+            const bool in = at + 32 * q < g.row_bytes;
             const int64_t from = in ? at + 32 * q : 0;      // (row starts are always there)
             fa[q] = *reinterpret_cast<const uint4*>(a + from);
             fb[q] = *reinterpret_cast<const uint4*>(b + from);
@@ -563,7 +549,7 @@ __global__ __launch_bounds__(256) void thin_sums_kernel(ThinRows g, int parts, i
     else sums[p * g.rows + row] = make_float4(s.m, s.s, s.t, 0.f);
 }
 // dz of such logits: a lane has four neighbouring classes
-template <typename T> __global__ __launch_bounds__(256) void thin_grads_kernel(ThinRows g, char* dz, int64_t dz_ld, int64_t dz_plane, int dz_classes) {
+__global__ __launch_bounds__(256) void thin_grads_kernel(ThinRows g, char* dz, int64_t dz_ld, int dz_classes) {
     const unsigned quads = (unsigned)dz_classes / 4, blocks = (quads + 255) / 256;
     const int64_t row = blockIdx.x / blocks;
     const unsigned quad = (blockIdx.x - (unsigned)row * blocks) * 256 + threadIdx.x;
@@ -577,7 +563,33 @@ template <typename T> __global__ __launch_bounds__(256) void thin_grads_kernel(T
 #pragma unroll
         for (int e = 0; e < 4; ++e) d[e] = c + e < g.classes ? grad.of(z[e], c + e == grad.target) : 0.f;
     }
-    store_dz<T>(dz + row * dz_ld + c * (int64_t)sizeof(T), dz_plane, d);
+    store_planes(dz + row * dz_ld, c, d);
+}
+// Sums of dz over kThinBiasRows rows at a time, [part][classes]: a block has 64 classes, eight to a thread.
+constexpr int kThinBiasRows = 512;
+__global__ __launch_bounds__(256) void thin_bias_kernel(const char* dz, int64_t dz_ld, int64_t rows, int64_t classes, float* db) {
+    __shared__ float part[32][65];
+    const int c = threadIdx.x & 7, r = threadIdx.x >> 3;
+    const int64_t first = (int64_t)blockIdx.x * 64, from = (int64_t)blockIdx.y * kThinBiasRows, to = min(from + kThinBiasRows, rows);
+    float sum[8] = {};
+    if (first + c * 8 < (classes + 15) / 16 * 16) {
+        const char* const at = dz + (first / 16 + c / 2) * 96 + (c & 1) * 16;
+        for (int64_t row = from + r; row < to; row += 32)
+#pragma unroll
+            for (int p = 0; p < 3; ++p) {
+                Vec16<bf16_t> v;
+                v.u = *reinterpret_cast<const uint4*>(at + row * dz_ld + p * 32);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] += bf16_to_f32(v.e[e]);
+            }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) part[r][c * 8 + e] = sum[e];
+    __syncthreads();
+    if (threadIdx.x >= 64 || first + threadIdx.x >= classes) return;
+    float s = 0.f;
+    for (int q = 0; q < 32; ++q) s += part[q][threadIdx.x];
+    db[blockIdx.y * classes + first + threadIdx.x] = s;
 }
 
 // ---- joins --------------------------------------------------------------------------------------------------------------
@@ -635,6 +647,37 @@ __global__ __launch_bounds__(256) void pad_rows_kernel(const T* __restrict__ src
     store_vec(dst + row * wide + c, v);
 }
 
+// rows of float32 as three planes, zeros up to whole groups of 16; a lane has four elements.  (What rounds to more than bf16
+// holds takes its largest number first.)
+__global__ __launch_bounds__(256) void split_rows_kernel(const float* __restrict__ src, int64_t ld, int64_t cols, char* __restrict__ dst, int64_t dst_ld, int64_t n) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= n) return;
+    const int64_t quads = dst_ld / 24, row = i / quads, c = (i - row * quads) * 4;
+    const float* const p = src + row * ld + c;
+    float v[4];
+    if (c + 4 <= cols) {
+        const Vec16<float> t = load_loose(p);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = t.e[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = c + e < cols ? p[e] : 0.f;
+    }
+    const float most = __uint_as_float(0x7f7f0000u);
+    char* const to = dst + row * dst_ld + (c >> 4) * 96 + (c & 15) * 2;
+    float high[4], rest[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        high[e] = fminf(fmaxf(v[e], -most), most);
+        rest[e] = v[e] - high[e];
+    }
+    *reinterpret_cast<uint2*>(to) = next_bf16(high);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) rest[e] += high[e];
+    *reinterpret_cast<uint2*>(to + 32) = next_bf16(rest);
+    *reinterpret_cast<uint2*>(to + 64) = next_bf16(rest);
+}
+
 // No rows: the gradients of weights and bias are sums of nothing.
 __global__ __launch_bounds__(256) void zero_rows_kernel(float* p, int64_t ld, int64_t cols, int64_t n) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -642,10 +685,11 @@ __global__ __launch_bounds__(256) void zero_rows_kernel(float* p, int64_t ld, in
 }
 
 constexpr int64_t kMiB = 1 << 20;
-constexpr int64_t kSmallTiles = 192;           // z of fewer tiles is formed in parts (thin_logits_kernel)
+constexpr int64_t kTile = 128, kBigTile = 256;
+constexpr int64_t kSmallTiles = 192;           // z of fewer 128x128 tiles is formed in parts (thin_logits_kernel)
 constexpr int64_t kDzBytes = 1024 * kMiB;      // of dz at a time
 constexpr int64_t kZeroAtOnce = 1ll << 30;     // elements of dw that one launch clears where there are no rows
-constexpr int64_t kMostAtOnce = 1 << 20;       // classes of it: 64 rows of dz are counted in 32 bits
+constexpr int64_t kMostAtOnce = 1 << 20;       // classes of it: offsets in a tile of dz are counted in 31 bits
 constexpr int64_t kWantBlocks = 512;           // two blocks of 128x128 per CU
 constexpr int64_t kChip = 256;                 // CUs: one block of 256x256 each
 constexpr int64_t kWantWaves = 2048;
@@ -654,56 +698,62 @@ constexpr int64_t kThinPart = 4096;            // classes of a part of a row, at
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
 
-// How a product of M x N outputs over `steps` steps is laid out: tiles of 256x256 where they fill most of the chip, the
-// reduction cut if need be, and little of them hangs over the edges; else of 128x128, the reduction cut towards two blocks
-// per CU, four steps to a cut at least.
-struct Layout { bool big; int cuts, per_cut; };
-Layout lay_out(int64_t M, int64_t N, int64_t steps, int esz, bool may_cut) {
+// How a product of M x N outputs over K is laid out: tiles of 256x256 where they fill most of the chip, the reduction cut
+// (into 1,024 elements at least) if need be, and little of them hangs over the edges; else of 128x128, the reduction cut
+// towards two blocks per CU, 256 elements to a cut at least.
+struct Layout { bool big; int64_t cuts, per_cut; };        // per_cut: elements of the reduction
+Layout lay_out(int64_t M, int64_t N, int64_t K, bool may_cut) {
     Layout l = {};
     const int64_t big = ceil_div(M, kBigTile) * ceil_div(N, kBigTile), tiles = ceil_div(M, kTile) * ceil_div(N, kTile);
-    const int64_t big_cuts = may_cut && big < kChip ? std::max<int64_t>(1, std::min<int64_t>(kChip / big, steps / 16)) : 1;
-    l.big = esz == 2 && big * big_cuts * 4 >= kChip * 3 && M * N * 4 >= big * kBigTile * kBigTile * 3;
+    const int64_t big_cuts = may_cut && big < kChip ? std::max<int64_t>(1, std::min<int64_t>(kChip / big, K / 1024)) : 1;
+    l.big = big * big_cuts * 4 >= kChip * 3 && M * N * 4 >= big * kBigTile * kBigTile * 3;
     int64_t want = 1;
     if (l.big) want = big_cuts;
-    else if (may_cut && tiles < kWantBlocks / 2) want = std::min<int64_t>(std::max<int64_t>(1, steps / 4), kWantBlocks / tiles);
-    l.per_cut = (int)ceil_div(steps, want);
-    l.cuts = (int)ceil_div(steps, l.per_cut);
+    else if (may_cut && tiles < kWantBlocks / 2) want = std::min<int64_t>(std::max<int64_t>(1, K / 256), kWantBlocks / tiles);
+    l.per_cut = round_up(ceil_div(K, want), 64);
+    l.cuts = ceil_div(K, l.per_cut);
     return l;
 }
 
 // everything a call does, from its sizes and alignments alone
 struct Plan {
     int esz;
+    bool thin;
+    // x and w as thin_logits_kernel reads them, and in bf16 everything: where they lie, or copied to whole 16 bytes
     int64_t wide;              // features up to whole 16 bytes
     bool pad_x, pad_w;
-    bool thin;
+    // float32: x and w as three planes, for the products on tiles
+    bool split;
+    int64_t split_ld;          // bytes
     int thin_cuts, thin_steps;         // of the reduction: cuts over blocks, steps of a wave
     int64_t z_ld;
     int thin_parts;
     int64_t thin_part;
-    int planes, dx_planes;
     int64_t chunk, chunks;     // of classes, in the backward pass
     Layout z, dx, dw;
-    int64_t z_tiles;           // of classes
+    int64_t z_tiles;           // of classes (forward), of rows (backward)
     // workspace
-    int64_t x_at, w_at, z_at, sums_at, target_at, dz_at, dz_ld, dz_plane, dx_at, dw_at, db_at, bytes;
+    int64_t x_at, w_at, xs_at, ws_at, z_at, sums_at, target_at, dz_at, dz_ld, dx_at, dw_at, db_at, bytes;
 };
 
 Plan plan_of(int dtype, int64_t rows, int64_t dim, int64_t classes, bool aligned_x, bool aligned_w, bool backward) {
     Plan p = {};
     p.esz = dtype == 1 ? 2 : 4;
-    const int64_t vec = 16 / p.esz, step = kStepBytes / p.esz;
-    p.wide = round_up(dim, vec);
-    p.pad_x = !aligned_x;
-    p.pad_w = !aligned_w;
     const int64_t tiles_r = ceil_div(rows, kTile), tiles_c = ceil_div(classes, kTile);
     int64_t o = 0;
     auto take = [&](int64_t bytes) { const int64_t at = o; o += round_up(bytes, 256); return at; };
+    p.thin = tiles_r * tiles_c < kSmallTiles;
+    p.wide = round_up(dim, 16 / p.esz);
+    p.pad_x = !aligned_x && (dtype == 1 || p.thin);
+    p.pad_w = !aligned_w && (dtype == 1 || p.thin);
+    p.split = dtype != 1 && (!p.thin || backward);
+    p.split_ld = round_up(dim, 16) * 6;
     p.x_at = take(p.pad_x ? rows * p.wide * p.esz : 0);
     p.w_at = take(p.pad_w ? classes * p.wide * p.esz : 0);
-    p.thin = tiles_r * tiles_c < kSmallTiles;
+    p.xs_at = take(p.split ? rows * p.split_ld : 0);
+    p.ws_at = take(p.split ? classes * p.split_ld : 0);
     if (p.thin) {
-        const int64_t steps = ceil_div(p.wide, step), small = ceil_div(rows, 32) * ceil_div(classes, 32);
+        const int64_t steps = ceil_div(p.wide * p.esz, kStepBytes), small = ceil_div(rows, 32) * ceil_div(classes, 32);
         const int64_t waves = std::max<int64_t>(4, std::min<int64_t>(kWantWaves / small, steps));
         p.thin_cuts = (int)std::max<int64_t>(1, waves / 4);
         p.thin_steps = (int)ceil_div(steps, p.thin_cuts * 4);
@@ -715,27 +765,25 @@ Plan plan_of(int dtype, int64_t rows, int64_t dim, int64_t classes, bool aligned
         p.z_at = take(p.thin_cuts * rows * p.z_ld * 4);
     }
     if (!backward) {
-        p.z = lay_out(classes, rows, 1, p.esz, false);
+        p.z = lay_out(classes, rows, 1, false);
         p.z_tiles = ceil_div(classes, p.z.big ? kBigTile : kTile);
         p.sums_at = take(p.thin ? (p.thin_parts > 1 ? p.thin_parts * rows * 16 : 0) : p.z_tiles * rows * 16);
         p.target_at = take(rows * 4);
     } else {
-        p.planes = dtype == 1 ? 3 : 1;
-        p.dx_planes = dtype == 1 ? 2 : 1;
-        const int64_t at_once = std::min(kMostAtOnce, std::max<int64_t>(1, kDzBytes / (rows * p.planes * p.esz * kTile)) * kTile);
+        const int64_t at_once = std::min(kMostAtOnce, std::max<int64_t>(1, kDzBytes / (rows * 6 * kTile)) * kTile);
         p.chunks = p.thin ? 1 : ceil_div(classes, at_once);
         p.chunk = round_up(ceil_div(classes, p.chunks), kTile);
         p.chunks = ceil_div(classes, p.chunk);
-        p.dz_ld = round_up(p.chunk * p.esz, 128);
-        p.dz_plane = rows * p.dz_ld;
-        p.dz_at = take(p.planes * p.dz_plane);
         const int64_t n = std::min(p.chunk, classes);
-        p.z = lay_out(n, rows, 1, p.esz, false);
-        p.dx = lay_out(rows, dim, ceil_div(n, step), p.esz, true);
-        p.dw = lay_out(n, dim, ceil_div(rows, step), p.esz, true);
+        p.dz_ld = round_up(n, 16) * 6;
+        p.dz_at = take(rows * p.dz_ld);
+        p.z = lay_out(n, rows, 1, false);
+        p.z_tiles = p.thin ? ceil_div(rows, kThinBiasRows) : ceil_div(rows, p.z.big ? kBigTile : kTile);
+        p.dx = lay_out(rows, dim, n, true);
+        p.dw = lay_out(n, dim, rows, true);
         p.dx_at = take(p.chunks * p.dx.cuts > 1 ? p.chunks * p.dx.cuts * rows * dim * 4 : 0);
-        p.dw_at = take(p.dw.cuts > 1 ? p.dw.cuts * p.chunk * dim * 4 : 0);
-        p.db_at = take(p.dw.cuts > 1 ? p.dw.cuts * p.chunk * 4 : 0);
+        p.dw_at = take(p.dw.cuts > 1 ? p.dw.cuts * n * dim * 4 : 0);
+        p.db_at = take(p.z_tiles > 1 ? p.z_tiles * n * 4 : 0);
     }
     p.bytes = o;
     return p;
@@ -745,20 +793,46 @@ bool lies_aligned(const void* p, int64_t ld, int64_t dim, int esz) {
     return (uintptr_t)p % 16 == 0 && ld * esz % 16 == 0 && dim * esz % 16 == 0 && ld * esz <= (1 << 23);
 }
 
-template <typename T> Operand padded(const void* src, int64_t ld, int64_t rows, int64_t dim, const Plan& p, bool pad, int64_t at, char* work, hipStream_t st) {
-    if (!pad) return Operand{(const char*)src, ld * p.esz, rows};
+// x or w as Plan says thin_logits_kernel reads it
+template <typename T> Matrix padded(const void* src, int64_t ld, int64_t rows, int64_t dim, const Plan& p, bool pad, int64_t at, char* work, hipStream_t st) {
+    if (!pad) return Matrix{(const char*)src, ld * p.esz, rows};
     const int64_t n = rows * (p.wide * p.esz / 16);
     ProfScope ps("classifier_pad", 0.0, (double)rows * (dim + p.wide) * p.esz, st);
     hipLaunchKernelGGL((pad_rows_kernel<T>), dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, st, (const T*)src, ld, dim, (T*)(work + at), p.wide, n);
-    return Operand{work + at, p.wide * p.esz, rows};
+    return Matrix{work + at, p.wide * p.esz, rows};
 }
+// x and w as operands whose reduction lies along them, in bf16 from their matrices
+struct Inputs { Matrix x, w; Operand xo, wo; };
+template <typename T> Inputs inputs_of(const ClassifierCall& c, const Plan& p, char* work, hipStream_t st) {
+    Inputs in = {};
+    if (sizeof(T) == 2 || p.thin) {
+        in.x = padded<T>(c.x, c.ldx, c.rows, c.dim, p, p.pad_x, p.x_at, work, st);
+        in.w = padded<T>(c.w, c.ldw, c.classes, c.dim, p, p.pad_w, p.w_at, work, st);
+    }
+    if (sizeof(T) == 2) {
+        in.xo = Operand{in.x.p, in.x.ld, c.rows, p.wide, 1};
+        in.wo = Operand{in.w.p, in.w.ld, c.classes, p.wide, 1};
+    } else if (p.split) {
+        auto split = [&](const void* src, int64_t ld, int64_t rows, int64_t at) {
+            const int64_t n = rows * (p.split_ld / 24);
+            ProfScope ps("classifier_split", 0.0, (4.0 * c.dim + p.split_ld) * rows, st);
+            hipLaunchKernelGGL(split_rows_kernel, dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, st, (const float*)src, ld, c.dim, work + at, p.split_ld, n);
+            return Operand{work + at, p.split_ld, rows, round_up(c.dim, 16), 3};
+        };
+        in.xo = split(c.x, c.ldx, c.rows, p.xs_at);
+        in.wo = split(c.w, c.ldw, c.classes, p.ws_at);
+    }
+    return in;
+}
+// the same memory with its lines the reduction: `rows` outputs (up to whole pieces) by `k` lines
+Operand across(const Operand& o, int64_t rows, int64_t k) { return Operand{o.p, o.ld, rows, k, o.stored}; }
 
-template <typename T> ThinRows thin_forward(const Operand& x, const Operand& w, const float* bias, const RowFacts& facts, const Plan& p, char* work, hipStream_t st) {
+template <typename T> ThinRows thin_forward(const Matrix& x, const Matrix& w, const float* bias, const RowFacts& facts, const Plan& p, char* work, hipStream_t st) {
     ThinArgs t = {};
     t.w = w;
     t.x = x;
-    t.k = p.wide;
-    t.steps = (int)ceil_div(p.wide * p.esz, kStepBytes);
+    t.row_bytes = p.wide * p.esz;
+    t.steps = (int)ceil_div(t.row_bytes, kStepBytes);
     t.steps_per_wave = p.thin_steps;
     t.tiles_m = (int)ceil_div(w.rows, 32);
     t.tiles_n = (int)ceil_div(x.rows, 32);
@@ -769,58 +843,49 @@ template <typename T> ThinRows thin_forward(const Operand& x, const Operand& w, 
     return ThinRows{t.z, p.z_ld, x.rows, w.rows, p.thin_cuts, bias, facts};
 }
 
-GemmArgs product_of(const Operand& a, const Operand& b, int64_t a_k, int64_t b_k, int esz, bool big) {
-    GemmArgs g = {};
-    g.a = a;
-    g.b = b;
-    g.a_k = a_k;
-    g.b_k = b_k;
-    g.planes = 1;
-    g.steps = g.steps_per_cut = (int)ceil_div(a_k * esz, kStepBytes);
-    g.tiles_m = (int)ceil_div(a.rows, big ? kBigTile : kTile);
-    g.tiles_n = (int)ceil_div(b.rows, big ? kBigTile : kTile);
+// a by b, `cut` elements of the reduction to a block, on tiles as laid out
+template <Want WANT, int PA, int PB, bool A_ALONG, bool B_ALONG, typename OUT> void launch_gemm(GemmArgs& g, int64_t cut, bool big, hipStream_t st) {
+    constexpr int KS = Steps<PA, PB>::KS;
+    const int64_t side = big ? kBigTile : kTile;
+    g.steps = (int)ceil_div(g.a.k, KS);
+    g.steps_per_cut = (int)std::min<int64_t>(g.steps, cut / KS);       // (a cut is a multiple of 64)
+    g.tiles_m = (int)ceil_div(g.a.rows, side);
+    g.tiles_n = (int)ceil_div(g.b.rows, side);
     g.group = big ? 4 : 8;
-    return g;
+    const dim3 grid((unsigned)(g.tiles_m * g.tiles_n * ceil_div(g.steps, g.steps_per_cut)));
+    if (big) hipLaunchKernelGGL((gemm_kernel<WANT, PA, PB, A_ALONG, B_ALONG, OUT, Shape256>), grid, dim3(512), 0, st, g);
+    else hipLaunchKernelGGL((gemm_kernel<WANT, PA, PB, A_ALONG, B_ALONG, OUT, Shape128>), grid, dim3(256), 0, st, g);
 }
-
-template <typename T, Want WANT, bool A_ALONG, bool B_ALONG, typename OUT> void launch_gemm(const GemmArgs& g, int cuts, bool big, hipStream_t st) {
-    const dim3 grid((unsigned)(g.tiles_m * g.tiles_n * cuts));
-    if constexpr (sizeof(T) == 2) {
-        if (big) {
-            hipLaunchKernelGGL((gemm_kernel<T, WANT, A_ALONG, B_ALONG, OUT, Shape256>), grid, dim3(512), 0, st, g);
-            return;
-        }
-    }
-    hipLaunchKernelGGL((gemm_kernel<T, WANT, A_ALONG, B_ALONG, OUT, Shape128>), grid, dim3(256), 0, st, g);
-}
+constexpr int64_t kWhole = 1ll << 30;          // no cuts
 
 template <typename T> void forward(const ClassifierCall& c, const ClassifierOut& out, hipStream_t st) {
+    constexpr int P = sizeof(T) == 2 ? 1 : 3;
     const Plan p = plan_of(c.dtype, c.rows, c.dim, c.classes, lies_aligned(c.x, c.ldx, c.dim, sizeof(T)), lies_aligned(c.w, c.ldw, c.dim, sizeof(T)), false);
     char* const work = (char*)c.work;
-    const Operand x = padded<T>(c.x, c.ldx, c.rows, c.dim, p, p.pad_x, p.x_at, work, st);
-    const Operand w = padded<T>(c.w, c.ldw, c.classes, c.dim, p, p.pad_w, p.w_at, work, st);
+    const Inputs in = inputs_of<T>(c, p, work, st);
     RowFacts facts = {};
     facts.targets = c.targets;
     const RowResults res = {out.log_prob, out.entropy, out.lse};
     float4* const sums = (float4*)(work + p.sums_at);
     float* const target_z = (float*)(work + p.target_at);
-    int64_t tiles;
+    int64_t tiles = p.z_tiles;
     if (p.thin) {
-        const ThinRows z = thin_forward<T>(x, w, c.bias, facts, p, work, st);
+        const ThinRows z = thin_forward<T>(in.x, in.w, c.bias, facts, p, work, st);
         ProfScope ps("classifier_thin_sums", 0.0, 4.0 * p.thin_cuts * c.rows * c.classes, st);
         hipLaunchKernelGGL(thin_sums_kernel, dim3((unsigned)(c.rows * p.thin_parts)), dim3(256), 0, st, z, p.thin_parts, p.thin_part, sums, target_z, res);
         tiles = p.thin_parts;
         if (tiles == 1) return;
     } else {
-        GemmArgs g = product_of(w, x, p.wide, p.wide, p.esz, p.z.big);
+        GemmArgs g = {};
+        g.a = in.wo;
+        g.b = in.xo;
         g.bias = c.bias;
         g.classes = c.classes;
         g.facts = facts;
         g.sums = sums;
         g.target_z = target_z;
-        tiles = g.tiles_m;
         ProfScope ps("classifier_sums", 2.0 * c.rows * c.classes * c.dim, (double)(c.rows + c.classes) * c.dim * p.esz, st);
-        launch_gemm<T, SUMS, true, true, float>(g, 1, p.z.big, st);
+        launch_gemm<SUMS, P, P, true, true, float>(g, kWhole, p.z.big, st);
     }
     ProfScope ps("classifier_join", 0.0, 16.0 * tiles * c.rows, st);
     hipLaunchKernelGGL(classifier_join_kernel, dim3((unsigned)ceil_div(c.rows, 32)), dim3(256), 0, st, sums, tiles, c.rows, c.targets, c.classes, target_z, res);
@@ -833,23 +898,33 @@ template <typename OUT> void sum_slots(const float* part, int64_t slots, int64_t
 }
 
 template <typename T> void backward(const ClassifierCall& c, const ClassifierGrads& d, hipStream_t st) {
+    constexpr int P = sizeof(T) == 2 ? 1 : 3;
     const Plan p = plan_of(c.dtype, c.rows, c.dim, c.classes, lies_aligned(c.x, c.ldx, c.dim, sizeof(T)), lies_aligned(c.w, c.ldw, c.dim, sizeof(T)), true);
     char* const work = (char*)c.work;
-    const Operand x = padded<T>(c.x, c.ldx, c.rows, c.dim, p, p.pad_x, p.x_at, work, st);
-    const Operand w = padded<T>(c.w, c.ldw, c.classes, c.dim, p, p.pad_w, p.w_at, work, st);
+    const Inputs in = inputs_of<T>(c, p, work, st);
     const RowFacts facts = {c.targets, d.lse, d.entropy, d.dlog_prob, d.dentropy};
     char* const dz = work + p.dz_at;
     const int64_t slots = p.chunks * p.dx.cuts;
-    const int row_bytes = (int)(p.wide * p.esz);
     for (int64_t q = 0; q < p.chunks; ++q) {
-        const int64_t from = q * p.chunk, n = std::min(p.chunk, c.classes - from), cols = round_up(n, 16 / p.esz);
-        const Operand wq = {w.p + from * w.ld, w.ld, n};
+        const int64_t from = q * p.chunk, n = std::min(p.chunk, c.classes - from), cols = round_up(n, 16);
+        Operand wq = in.wo;
+        wq.p += from * wq.ld;
+        wq.rows = n;
+        float* const db = d.dbias == nullptr ? nullptr : p.z_tiles > 1 ? (float*)(work + p.db_at) : d.dbias + from;
         if (p.thin) {
-            const ThinRows z = thin_forward<T>(x, w, c.bias, facts, p, work, st);
-            ProfScope ps("classifier_thin_grads", 0.0, (4.0 * p.thin_cuts + p.planes * p.esz) * c.rows * c.classes, st);
-            hipLaunchKernelGGL((thin_grads_kernel<T>), dim3((unsigned)(c.rows * ceil_div(cols / 4, 256))), dim3(256), 0, st, z, dz, p.dz_ld, p.dz_plane, (int)cols);
+            const ThinRows z = thin_forward<T>(in.x, in.w, c.bias, facts, p, work, st);
+            {
+                ProfScope ps("classifier_thin_grads", 0.0, (4.0 * p.thin_cuts + 6.0) * c.rows * c.classes, st);
+                hipLaunchKernelGGL(thin_grads_kernel, dim3((unsigned)(c.rows * ceil_div(cols / 4, 256))), dim3(256), 0, st, z, dz, p.dz_ld, (int)cols);
+            }
+            if (db != nullptr) {
+                ProfScope ps("classifier_thin_bias", 0.0, 6.0 * c.rows * c.classes, st);
+                hipLaunchKernelGGL(thin_bias_kernel, dim3((unsigned)ceil_div(n, 64), (unsigned)p.z_tiles), dim3(256), 0, st, dz, p.dz_ld, c.rows, n, db);
+            }
         } else {
-            GemmArgs g = product_of(wq, x, p.wide, p.wide, p.esz, p.z.big);
+            GemmArgs g = {};
+            g.a = wq;
+            g.b = in.xo;
             g.bias = c.bias;
             g.first_class = from;
             g.classes = from + n;
@@ -857,58 +932,45 @@ template <typename T> void backward(const ClassifierCall& c, const ClassifierGra
             g.facts = facts;
             g.dz = dz;
             g.dz_ld = p.dz_ld;
-            g.dz_plane = p.dz_plane;
             g.dz_classes = (int)cols;
-            ProfScope ps("classifier_dz", 2.0 * c.rows * n * c.dim, (double)(c.rows + n) * c.dim * p.esz + (double)p.planes * p.esz * c.rows * n, st);
-            launch_gemm<T, GRADS, true, true, float>(g, 1, p.z.big, st);
+            g.db = db;
+            g.db_ld = n;
+            ProfScope ps("classifier_dz", 2.0 * c.rows * n * c.dim, (double)(c.rows + n) * c.dim * p.esz + 6.0 * c.rows * n, st);
+            launch_gemm<GRADS, P, P, true, true, float>(g, kWhole, p.z.big, st);
         }
+        if (db != nullptr && p.z_tiles > 1) sum_slots<float>(db, p.z_tiles, 1, n, d.dbias + from, n, st);
         {
-            GemmArgs g = product_of(Operand{dz, p.dz_ld, c.rows}, Operand{wq.p, wq.ld, c.dim}, cols, n, p.esz, p.dx.big);
-            g.a_plane = p.dz_plane;
-            g.planes = p.dx_planes;
-            g.b_row_bytes = row_bytes;
-            g.steps_per_cut = p.dx.per_cut;
-            const int cuts = (int)ceil_div(g.steps, g.steps_per_cut);
-            ProfScope ps("classifier_dx", 2.0 * c.rows * n * c.dim, (double)p.dx_planes * p.esz * c.rows * n + (double)p.esz * (n + c.rows) * c.dim, st);
+            GemmArgs g = {};
+            g.a = Operand{dz, p.dz_ld, c.rows, cols, 3};
+            g.b = across(wq, c.dim, n);
+            ProfScope ps("classifier_dx", 2.0 * c.rows * n * c.dim, 6.0 * c.rows * n + (double)p.esz * (n + c.rows) * c.dim, st);
             if (slots > 1) {
-                // (the last chunk may have fewer cuts: the slots it leaves out are not summed, see below)
                 g.out = (float*)(work + p.dx_at) + q * p.dx.cuts * c.rows * c.dim;
                 g.out_ld = c.dim;
                 g.out_cut = c.rows * c.dim;
-                launch_gemm<T, PRODUCT, true, false, float>(g, cuts, p.dx.big, st);
+                launch_gemm<PRODUCT, P == 1 ? 2 : 3, P, true, false, float>(g, p.dx.per_cut, p.dx.big, st);
             } else {
                 g.out = d.dx;
                 g.out_ld = d.lddx;
-                launch_gemm<T, PRODUCT, true, false, T>(g, cuts, p.dx.big, st);
-            }
-            if (q + 1 == p.chunks && slots > 1) {
-                const int64_t used = (p.chunks - 1) * p.dx.cuts + cuts;
-                sum_slots<T>((const float*)(work + p.dx_at), used, c.rows, c.dim, (T*)d.dx, d.lddx, st);
+                launch_gemm<PRODUCT, P == 1 ? 2 : 3, P, true, false, T>(g, kWhole, p.dx.big, st);
             }
         }
+        // (the last piece of the classes may have fewer cuts: the slots that it leaves out are not summed)
+        if (q + 1 == p.chunks && slots > 1)
+            sum_slots<T>((const float*)(work + p.dx_at), (p.chunks - 1) * p.dx.cuts + ceil_div(n, p.dx.per_cut), c.rows, c.dim, (T*)d.dx, d.lddx, st);
         {
-            GemmArgs g = product_of(Operand{dz, p.dz_ld, n}, Operand{x.p, x.ld, c.dim}, c.rows, c.rows, p.esz, p.dw.big);
-            g.a_plane = p.dz_plane;
-            g.planes = p.planes;
-            g.a_row_bytes = (int)(cols * p.esz);
-            g.b_row_bytes = row_bytes;
-            g.steps_per_cut = p.dw.per_cut;
+            GemmArgs g = {};
+            g.a = Operand{dz, p.dz_ld, n, c.rows, 3};
+            g.b = across(in.xo, c.dim, c.rows);
             const bool cut = p.dw.cuts > 1;
             g.out = cut ? (float*)(work + p.dw_at) : d.dw + from * d.lddw;
             g.out_ld = cut ? c.dim : d.lddw;
             g.out_cut = n * c.dim;
-            if (d.dbias != nullptr) {
-                g.dbias = cut ? (float*)(work + p.db_at) : d.dbias + from;
-                g.dbias_cut = n;
-            }
             {
-                ProfScope ps("classifier_dw", 2.0 * c.rows * n * c.dim, (double)p.planes * p.esz * c.rows * n + (double)p.esz * c.rows * c.dim + 4.0 * n * c.dim, st);
-                launch_gemm<T, PRODUCT, false, false, float>(g, p.dw.cuts, p.dw.big, st);
+                ProfScope ps("classifier_dw", 2.0 * c.rows * n * c.dim, 6.0 * c.rows * n + (double)p.esz * c.rows * c.dim + 4.0 * n * c.dim, st);
+                launch_gemm<PRODUCT, 3, P, false, false, float>(g, p.dw.per_cut, p.dw.big, st);
             }
-            if (cut) {
-                sum_slots<float>((const float*)(work + p.dw_at), p.dw.cuts, n, c.dim, d.dw + from * d.lddw, d.lddw, st);
-                if (d.dbias != nullptr) sum_slots<float>((const float*)(work + p.db_at), p.dw.cuts, 1, n, d.dbias + from, n, st);
-            }
+            if (cut) sum_slots<float>((const float*)(work + p.dw_at), p.dw.cuts, n, c.dim, d.dw + from * d.lddw, d.lddw, st);
         }
     }
 }

@@ -123,7 +123,7 @@ int32_t edl_log_probs_backward(int32_t dtype, const void* dev_logits, int64_t ld
 static int32_t check_classifier(int32_t dtype, int64_t rows, int64_t dim, int64_t classes) {
     if (!known_dtype(dtype)) return EDL_EINVAL;
     if (rows < 0 || dim <= 0 || classes <= 0) { set_error("rows must not be negative, dim and classes positive"); return EDL_EINVAL; }
-    if (rows > kMaxRows || dim > kMaxDim || classes > kMaxClasses || rows * dim > (1ll << 31) || classes * dim > (1ll << 34) ||
+    if (rows > kMaxRows || dim > kMaxDim || classes > kMaxClasses || rows * dim > (1ll << 31) || classes * dim > (1ll << 33) ||
         ((rows + 127) / 128) * ((classes + 127) / 128) > kMaxTiles) {
         set_error("%lld rows of %lld features for %lld classes are too many", (long long)rows, (long long)dim, (long long)classes);
         return EDL_ERANGE;
