@@ -51,14 +51,20 @@ template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_
 
 // One operand of a product: element (r, k) of `rows` by `k` of the reduction, bf16.  along: row r's reduction lies at
 // p + r * ld; across: k's rows lie at p + k * ld.  A line's elements follow each other, or, of an operand of three planes, in
-// groups of 16: the group's first plane, second, third (32 bytes each).  p and ld are multiples of 16 bytes, a line's elements
-// whole pieces of 8 (of planes: groups of 16) with zeros past the operand's.
+// groups of 64: the group's first plane, second, third (a line of the caches each).  p and ld are multiples of 16 bytes, a line's
+// elements whole pieces of 8 with zeros past the operand's.
+constexpr int kGroup = 64;
+constexpr int64_t kGroupBytes = 3 * 2 * kGroup;
+__host__ __device__ inline int64_t planes_bytes(int64_t n) { return (n + kGroup - 1) / kGroup * kGroupBytes; }
+// where element c of such a line has its first plane; the others follow 2 kGroup bytes apart
+__host__ __device__ inline int64_t plane_at(int64_t c) { return c / kGroup * kGroupBytes + c % kGroup * 2; }
 struct Operand {
     const char* p;
     int64_t ld;                // bytes
     int64_t rows, k;
     int stored;                // planes in memory: 1 or 3
-    __host__ __device__ int64_t line_bytes(int64_t n) const { return stored == 1 ? (n + 7) / 8 * 16 : (n + 15) / 16 * 32 * stored; }
+    __host__ __device__ int64_t line_bytes(int64_t n) const { return stored == 1 ? (n + 7) / 8 * 16 : planes_bytes(n); }
+    __host__ __device__ int64_t at(int64_t c) const { return stored == 1 ? 2 * c : plane_at(c); }       // of a line's element
 };
 
 // Tiles of W rows and one reduction step of KS elements in LDS, one for each of the first P planes.
@@ -75,10 +81,10 @@ template <bool ALONG, int W, int P, int KS, int THREADS> struct Tile {
 
     unsigned offset[LOADS];      // this lane's, from the step's start
     int piece_k;                 // along: which of the step's elements this lane's pieces hold first
-    // of the step that is loaded next: where it starts, bytes of the operand from there on, elements of the reduction
-    const char* next;
-    int64_t left, stride;
-    int k_left;
+    // of the step that is loaded next: elements of the reduction before it, and with the operand's tile and its bytes where it starts
+    int64_t k_at;
+    const char* tile;
+    int64_t bytes;
     // of the step that is being loaded
     i32x4 extent;
     int k_here;
@@ -87,30 +93,25 @@ template <bool ALONG, int W, int P, int KS, int THREADS> struct Tile {
     __device__ __forceinline__ static int piece_of(int piece, int row) { return piece ^ ((row * PIECES / 16) & (PIECES - 1)); }
 
     __device__ __forceinline__ void init(const Operand& o, int64_t first_row) {
-        stride = ALONG ? (int64_t)KS * 2 * o.stored : KS * o.ld;
+        tile = o.p + (ALONG ? first_row * o.ld : o.at(first_row));
+        bytes = ALONG ? (o.rows - first_row - 1) * o.ld + o.line_bytes(o.k) : (o.k - 1) * o.ld + o.line_bytes(o.rows) - o.at(first_row);
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int slot = i * THREADS + (int)threadIdx.x, plane = slot / (PLANE / 16), line = slot % (PLANE / 16) / PIECES, s = slot % PIECES;
             const int piece = ALONG ? piece_of(s, line) : pair_of(s >> 1, line) << 1 | (s & 1);
-            const unsigned at = (unsigned)(line * o.ld) + ((piece >> 1) * o.stored + plane) * 32 + (piece & 1) * 16;
+            // (a step along does not cross a group: KS divides it)
+            const unsigned at = (unsigned)(line * o.ld) + plane * 2 * kGroup + (unsigned)(ALONG ? piece * 16 : o.at(piece * 8));
             offset[i] = ALONG || first_row + piece * 8 < o.rows ? at : kNowhere;
             if (ALONG && i == 0) piece_k = piece * 8;
         }
     }
-    __device__ __forceinline__ void start(const Operand& o, int64_t first_row, int64_t step) {
-        next = o.p + (ALONG ? first_row * o.ld : first_row * 2 * o.stored) + step * stride;
-        left = ALONG ? (o.rows - first_row - 1) * o.ld + o.line_bytes(o.k) - step * stride
-                     : (o.k - step * KS - 1) * o.ld + o.line_bytes(o.rows) - first_row * 2 * o.stored;
-        k_left = (int)min(o.k - step * KS, (int64_t)0x7fffffff);
-    }
     // Turns to the next step; there: false past the last one (its loads bring zeros into a stage that nobody reads, so that
     // loads can be counted).
-    __device__ __forceinline__ void turn(bool there) {
-        extent = extent_of(next, there ? left : 0);
-        k_here = k_left;
-        next += stride;
-        left -= stride;
-        k_left -= KS;
+    __device__ __forceinline__ void turn(const Operand& o, bool there) {
+        const int64_t at = ALONG ? o.at(k_at) : k_at * o.ld;
+        extent = extent_of(tile + at, there ? bytes - at : 0);
+        k_here = (int)min(o.k - k_at, (int64_t)KS);
+        k_at += KS;
     }
     // the i-th of this step's loads
     __device__ __forceinline__ void load(int i, unsigned lds) const {
@@ -161,9 +162,9 @@ __device__ __forceinline__ uint2 next_bf16(float (&v)[4]) {
 }
 // four neighbouring elements, the first of them number c (a multiple of 4), of a line of three planes
 __device__ __forceinline__ void store_planes(char* line, int64_t c, float (&v)[4]) {
-    char* const p = line + (c >> 4) * 96 + (c & 15) * 2;
+    char* const p = line + plane_at(c);
 #pragma unroll
-    for (int q = 0; q < 3; ++q) *reinterpret_cast<uint2*>(p + q * 32) = next_bf16(v);
+    for (int q = 0; q < 3; ++q) *reinterpret_cast<uint2*>(p + q * 2 * kGroup) = next_bf16(v);
 }
 
 enum Want { SUMS, GRADS, PRODUCT };     // of z: sums over classes, dz; of the others: the product itself
@@ -180,7 +181,7 @@ struct GemmArgs {
     float* target_z;
     char* dz;                  // [rows][dz_ld bytes] of the classes from first_class on, three planes
     int64_t dz_ld;
-    int dz_classes;            // of whole groups (zeros past the last class)
+    int dz_classes;            // up to whole pairs of pieces (zeros past the last class)
     float* db;                 // [tile of rows][db_ld] sums of dz; null: not wanted
     int64_t db_ld;
     // products
@@ -229,13 +230,12 @@ __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmAr
     TB tb;
     ta.init(g.a, m0);
     tb.init(g.b, n0);
-    ta.start(g.a, m0, first);
-    tb.start(g.b, n0, first);
+    ta.k_at = tb.k_at = (int64_t)first * KS;
     int asked = 0, to = 0;                                  // steps asked for, and the stage of the one being loaded
     auto turn = [&]() {
         const bool there = asked < all;
-        ta.turn(there);
-        tb.turn(there);
+        ta.turn(g.a, there);
+        tb.turn(g.b, there);
         if (asked > 0) to = to + 1 == STAGES ? 0 : to + 1;
         ++asked;
     };
@@ -399,7 +399,7 @@ __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmAr
                 }
                 __syncthreads();
                 if (wanted) {
-                    char* const out = g.dz + n0 * g.dz_ld + (m0 / 16 + c / 2) * 96 + p * 32 + (c & 1) * 16;
+                    char* const out = g.dz + n0 * g.dz_ld + plane_at(m0 + c * 8) + p * 2 * kGroup;
                     for (int r = threadIdx.x / PIECES; r < rows; r += ROWS) {
                         Vec16<bf16_t> v;
                         v.u = *reinterpret_cast<const uint4*>(smem + (r * PIECES + (c ^ (r & (PIECES - 1)))) * 16);
@@ -573,12 +573,12 @@ __global__ __launch_bounds__(256) void thin_bias_kernel(const char* dz, int64_t 
     const int64_t first = (int64_t)blockIdx.x * 64, from = (int64_t)blockIdx.y * kThinBiasRows, to = min(from + kThinBiasRows, rows);
     float sum[8] = {};
     if (first + c * 8 < (classes + 15) / 16 * 16) {
-        const char* const at = dz + (first / 16 + c / 2) * 96 + (c & 1) * 16;
+        const char* const at = dz + plane_at(first + c * 8);
         for (int64_t row = from + r; row < to; row += 32)
 #pragma unroll
             for (int p = 0; p < 3; ++p) {
                 Vec16<bf16_t> v;
-                v.u = *reinterpret_cast<const uint4*>(at + row * dz_ld + p * 32);
+                v.u = *reinterpret_cast<const uint4*>(at + row * dz_ld + p * 2 * kGroup);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum[e] += bf16_to_f32(v.e[e]);
             }
@@ -647,12 +647,12 @@ __global__ __launch_bounds__(256) void pad_rows_kernel(const T* __restrict__ src
     store_vec(dst + row * wide + c, v);
 }
 
-// rows of float32 as three planes, zeros up to whole groups of 16; a lane has four elements.  (What rounds to more than bf16
+// rows of float32 as three planes, zeros up to whole groups; a lane has four elements.  (What rounds to more than bf16
 // holds takes its largest number first.)
 __global__ __launch_bounds__(256) void split_rows_kernel(const float* __restrict__ src, int64_t ld, int64_t cols, char* __restrict__ dst, int64_t dst_ld, int64_t n) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= n) return;
-    const int64_t quads = dst_ld / 24, row = i / quads, c = (i - row * quads) * 4;
+    const int64_t quads = dst_ld / kGroupBytes * (kGroup / 4), row = i / quads, c = (i - row * quads) * 4;
     const float* const p = src + row * ld + c;
     float v[4];
     if (c + 4 <= cols) {
@@ -664,7 +664,7 @@ __global__ __launch_bounds__(256) void split_rows_kernel(const float* __restrict
         for (int e = 0; e < 4; ++e) v[e] = c + e < cols ? p[e] : 0.f;
     }
     const float most = __uint_as_float(0x7f7f0000u);
-    char* const to = dst + row * dst_ld + (c >> 4) * 96 + (c & 15) * 2;
+    char* const to = dst + row * dst_ld + plane_at(c);
     float high[4], rest[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -674,8 +674,8 @@ __global__ __launch_bounds__(256) void split_rows_kernel(const float* __restrict
     *reinterpret_cast<uint2*>(to) = next_bf16(high);
 #pragma unroll
     for (int e = 0; e < 4; ++e) rest[e] += high[e];
-    *reinterpret_cast<uint2*>(to + 32) = next_bf16(rest);
-    *reinterpret_cast<uint2*>(to + 64) = next_bf16(rest);
+    *reinterpret_cast<uint2*>(to + 2 * kGroup) = next_bf16(rest);
+    *reinterpret_cast<uint2*>(to + 4 * kGroup) = next_bf16(rest);
 }
 
 // No rows: the gradients of weights and bias are sums of nothing.
@@ -747,7 +747,7 @@ Plan plan_of(int dtype, int64_t rows, int64_t dim, int64_t classes, bool aligned
     p.pad_x = !aligned_x && (dtype == 1 || p.thin);
     p.pad_w = !aligned_w && (dtype == 1 || p.thin);
     p.split = dtype != 1 && (!p.thin || backward);
-    p.split_ld = round_up(dim, 16) * 6;
+    p.split_ld = planes_bytes(dim);
     p.x_at = take(p.pad_x ? rows * p.wide * p.esz : 0);
     p.w_at = take(p.pad_w ? classes * p.wide * p.esz : 0);
     p.xs_at = take(p.split ? rows * p.split_ld : 0);
@@ -775,7 +775,7 @@ Plan plan_of(int dtype, int64_t rows, int64_t dim, int64_t classes, bool aligned
         p.chunk = round_up(ceil_div(classes, p.chunks), kTile);
         p.chunks = ceil_div(classes, p.chunk);
         const int64_t n = std::min(p.chunk, classes);
-        p.dz_ld = round_up(n, 16) * 6;
+        p.dz_ld = planes_bytes(n);
         p.dz_at = take(rows * p.dz_ld);
         p.z = lay_out(n, rows, 1, false);
         p.z_tiles = p.thin ? ceil_div(rows, kThinBiasRows) : ceil_div(rows, p.z.big ? kBigTile : kTile);
@@ -814,7 +814,7 @@ template <typename T> Inputs inputs_of(const ClassifierCall& c, const Plan& p, c
         in.wo = Operand{in.w.p, in.w.ld, c.classes, p.wide, 1};
     } else if (p.split) {
         auto split = [&](const void* src, int64_t ld, int64_t rows, int64_t at) {
-            const int64_t n = rows * (p.split_ld / 24);
+            const int64_t n = rows * (p.split_ld / kGroupBytes * (kGroup / 4));
             ProfScope ps("classifier_split", 0.0, (4.0 * c.dim + p.split_ld) * rows, st);
             hipLaunchKernelGGL(split_rows_kernel, dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, st, (const float*)src, ld, c.dim, work + at, p.split_ld, n);
             return Operand{work + at, p.split_ld, rows, round_up(c.dim, 16), 3};
