@@ -308,36 +308,54 @@ __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmAr
                 }
         }
     } else {
-        // z: rows of the tile are classes, columns rows of x.  Class of element e of tile i: c0 + place(i, e); those from c0 + left
-        // on are none
+        // z: rows of the tile are classes, columns rows of x.  Class of element e of tile i: c0 + place(i, e).  Past the last class
+        // the bias is -inf, which masks it like any other.
         const int64_t c0 = g.first_class + m0 + wm * TM * 32 + 4 * (lane >> 5);
-        const int left = (int)min((int64_t)4096, g.classes - c0);
         auto place = [](int i, int e) { return 32 * i + 8 * (e >> 2) + (e & 3); };
-        float bias[TM][16];
+        float* const bias = reinterpret_cast<float*>(smem);
+        if (threadIdx.x < SIDE) {
+            const int64_t c = g.first_class + m0 + threadIdx.x;
+            bias[threadIdx.x] = c >= g.classes ? -INFINITY : g.bias != nullptr ? g.bias[c] : 0.f;
+        }
+        __syncthreads();
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) bias[i][e] = g.bias != nullptr && place(i, e) < left ? g.bias[c0 + place(i, e)] : 0.f;
+            for (int q = 0; q < 4; ++q) {
+                const float4 b = *reinterpret_cast<const float4*>(bias + (wm * TM + i) * 32 + 8 * q + 4 * (lane >> 5));
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    acc[i][j][4 * q] += b.x;
+                    acc[i][j][4 * q + 1] += b.y;
+                    acc[i][j][4 * q + 2] += b.z;
+                    acc[i][j][4 * q + 3] += b.w;
+                }
+            }
+        // where a row's target is among this lane's classes, or -1
+        auto place_of = [&](int64_t target) { return target >= c0 && target < min(c0 + TM * 32, g.classes) ? (int)(target - c0) : -1; };
         if constexpr (WANT == SUMS) {
-            float4* const part = reinterpret_cast<float4*>(smem);      // [wm][SIDE]
+            float4* const part = reinterpret_cast<float4*>(smem + SIDE * 4);      // [wm][SIDE]
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
                 const int col = (wn * TN + j) * 32 + (lane & 31);
                 const int64_t n = n0 + col;
                 const int64_t t = n < g.b.rows && g.facts.targets != nullptr ? g.facts.targets[n] : -1;
-                const int hot = t >= c0 && t < c0 + left ? (int)(t - c0) : -1;
+                const int hot = place_of(t);
                 SoftmaxSums s;
-                float zt = 0.f;
-                bool here = false;
 #pragma unroll
                 for (int i = 0; i < TM; ++i)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const float z = place(i, e) < left ? acc[i][j][e] + bias[i][e] : -INFINITY;
-                        acc[i][j][e] = z;
-                        s.m = fmaxf(s.m, z);
-                        if (place(i, e) == hot) { zt = z; here = true; }
-                    }
+                    for (int e = 0; e < 16; ++e) s.m = fmaxf(s.m, acc[i][j][e]);
+                if (__ballot(hot >= 0) != 0) {     // (few tiles hold a row's target)
+                    float zt = 0.f;
+                    bool here = false;
+#pragma unroll
+                    for (int i = 0; i < TM; ++i)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e)
+                            if (place(i, e) == hot) { zt = acc[i][j][e]; here = true; }
+                    if (here) g.target_z[n] = zt;
+                }
                 const float base = softmax_base(s);
 #pragma unroll
                 for (int i = 0; i < TM; ++i)
@@ -345,7 +363,6 @@ __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmAr
                     for (int e = 0; e < 16; ++e) softmax_add(s, acc[i][j][e], base);
                 softmax_join(s, softmax_shuffle(s, 32));
                 if (lane < 32) part[wm * SIDE + col] = make_float4(s.m, s.s, s.t, 0.f);
-                if (here) g.target_z[n] = zt;
             }
             __syncthreads();
             if (threadIdx.x < SIDE && n0 + threadIdx.x < g.b.rows) {
@@ -369,18 +386,18 @@ __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmAr
             for (int j = 0; j < TN; ++j) {
                 const int64_t n = n0 + (wn * TN + j) * 32 + (lane & 31);
                 const LogitGrad row = logit_grad(g.facts, min(n, g.b.rows - 1), g.all_classes);
-                const int hot = row.target >= c0 && row.target < c0 + left ? (int)(row.target - c0) : -1;
+                const int hot = place_of(row.target);
 #pragma unroll
                 for (int i = 0; i < TM; ++i)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) acc[i][j][e] = place(i, e) < left ? row.of(acc[i][j][e] + bias[i][e], place(i, e) == hot) : 0.f;
+                    for (int e = 0; e < 16; ++e) acc[i][j][e] = row.of(acc[i][j][e], place(i, e) == hot);
             }
             const int c = threadIdx.x % PIECES, rows = (int)min((int64_t)SIDE, g.b.rows - n0);
             const bool wanted = m0 + c * 8 < g.dz_classes;
             float total[8] = {};
 #pragma unroll
             for (int p = 0; p < 3; ++p) {
-                if (p > 0) __syncthreads();        // the plane before is out
+                __syncthreads();           // the biases are read, or the plane before is out
 #pragma unroll
                 for (int j = 0; j < TN; ++j) {
                     const int r = (wn * TN + j) * 32 + (lane & 31);
