@@ -138,16 +138,6 @@ template <bool ALONG, int W, int P, int KS, int THREADS> struct Tile {
     }
 };
 
-template <typename T> __device__ __forceinline__ void multiply(const uint4& a, const uint4& b, floatx16& c) {
-    if constexpr (sizeof(T) == 2) {
-        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-    } else {
-        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.x), __uint_as_float(b.x), c, 0, 0, 0);
-        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.y), __uint_as_float(b.y), c, 0, 0, 0);
-        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.z), __uint_as_float(b.z), c, 0, 0, 0);
-        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.w), __uint_as_float(b.w), c, 0, 0, 0);
-    }
-}
 // row of a 32x32 tile that element e of a lane's 16 stands for (its column is lane % 32)
 __device__ __forceinline__ int tile_row(int e, int lane) { return 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3); }
 
@@ -284,7 +274,8 @@ __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmAr
 #pragma unroll
                     for (int i = 0; i < TM; ++i)
 #pragma unroll
-                        for (int j = 0; j < TN; ++j) multiply<bf16_t>(fa[i], fb[b][j], acc[i][j]);
+                        for (int j = 0; j < TN; ++j) 
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fa[i]), __builtin_bit_cast(bf16x8, fb[b][j]), acc[i][j], 0, 0, 0);
                 const int group = q * PA + a;
 #pragma unroll
                 for (int i = group * LOADS / GROUPS; i < (group + 1) * LOADS / GROUPS; ++i) load(i);
@@ -443,26 +434,23 @@ __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmAr
 }
 
 // ---- few tiles ----------------------------------------------------------------------------------------------------------
-// Where z has too few tiles to fill the chip it is formed in 32x32 tiles with the reduction cut as well, over a block's four
-// waves and over blocks, and its float32 parts are stored: [cut][rows][z_ld].  Fragments come straight from memory (L2: a
-// tile is used by few); what that bounds is the latency of the chain of loads, so each wave has eight in flight.
+// Where z has too few tiles to fill the chip its reduction is cut as well and its float32 parts are stored: [cut][rows][z_ld].
+// They come from gemm_kernel, or, of up to 32 float32 rows (which would not repay the copies that it needs), from this one: a
+// wave has 32 rows of w and its part of the reduction, on float32 matrix instructions, fragments straight from memory.
 constexpr int kStepBytes = 128;        // of a reduction step
 struct Matrix { const char* p; int64_t ld, rows; };        // ld in bytes; 16-byte aligned
 struct ThinArgs {
     Matrix w, x;
     int64_t row_bytes;         // whole 16 bytes
-    int steps, steps_per_wave, tiles_m, tiles_n;
+    int steps, steps_per_wave, tiles;
     float* z;
     int64_t z_ld;
 };
-template <typename T> __global__ __launch_bounds__(256) void thin_logits_kernel(ThinArgs g) {
+__global__ __launch_bounds__(256) void thin_logits_kernel(ThinArgs g) {
     __shared__ float part[4][16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    unsigned l = blockIdx.x;
-    const int tn = (int)(l % (unsigned)g.tiles_n);
-    l /= (unsigned)g.tiles_n;
-    const int tm = (int)(l % (unsigned)g.tiles_m), cut = (int)(l / (unsigned)g.tiles_m);
-    const int64_t m = min((int64_t)tm * 32 + (lane & 31), g.w.rows - 1), n = min((int64_t)tn * 32 + (lane & 31), g.x.rows - 1);
+    const int tm = (int)(blockIdx.x % (unsigned)g.tiles), cut = (int)(blockIdx.x / (unsigned)g.tiles);
+    const int64_t m = min((int64_t)tm * 32 + (lane & 31), g.w.rows - 1), n = min((int64_t)(lane & 31), g.x.rows - 1);
     const int first = (cut * 4 + wave) * g.steps_per_wave, last = min(first + g.steps_per_wave, g.steps);
     int64_t at = (int64_t)first * kStepBytes + 16 * (lane >> 5);
     const char* const a = g.w.p + m * g.w.ld;
@@ -481,12 +469,17 @@ template <typename T> __global__ __launch_bounds__(256) void thin_logits_kernel(
             if (!in) fa[q] = fb[q] = make_uint4(0, 0, 0, 0);
         }
 #pragma unroll
-        for (int q = 0; q < 4; ++q) multiply<T>(fa[q], fb[q], acc);
+        for (int q = 0; q < 4; ++q) {
+            acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(fa[q].x), __uint_as_float(fb[q].x), acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(fa[q].y), __uint_as_float(fb[q].y), acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(fa[q].z), __uint_as_float(fb[q].z), acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(fa[q].w), __uint_as_float(fb[q].w), acc, 0, 0, 0);
+        }
     }
 #pragma unroll
     for (int e = 0; e < 16; ++e) part[wave][e][lane] = acc[e];
     __syncthreads();
-    const int64_t row = (int64_t)tn * 32 + (lane & 31);
+    const int64_t row = lane & 31;
     if (row >= g.x.rows) return;
     float v[4];
 #pragma unroll
@@ -506,9 +499,12 @@ struct ThinRows {
 };
 // four neighbouring logits (classes past the last: whatever lies there)
 __device__ __forceinline__ float4 thin_logits(const ThinRows& g, int64_t row, int64_t c) {
-    float4 v = *reinterpret_cast<const float4*>(g.z + row * g.z_ld + c);
-    for (int q = 1; q < g.cuts; ++q) {
-        const float4 p = *reinterpret_cast<const float4*>(g.z + (q * g.rows + row) * g.z_ld + c);
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float* const z = g.z + row * g.z_ld + c;
+    const int64_t cut = g.rows * g.z_ld;
+#pragma unroll 8
+    for (int q = 0; q < g.cuts; ++q) {         // (unrolled: the loads do not wait for each other)
+        const float4 p = *reinterpret_cast<const float4*>(z + q * cut);
         v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
     }
     if (g.bias != nullptr) {
@@ -742,7 +738,9 @@ struct Plan {
     // float32: x and w as three planes, for the products on tiles
     bool split;
     int64_t split_ld;          // bytes
-    int thin_cuts, thin_steps;         // of the reduction: cuts over blocks, steps of a wave
+    bool narrow;               // thin_logits_kernel
+    int thin_cuts, thin_steps;         // of the reduction: cuts over blocks, steps of a wave of it
+    Layout thin_z;
     int64_t z_ld;
     int thin_parts;
     int64_t thin_part;
@@ -761,20 +759,26 @@ Plan plan_of(int dtype, int64_t rows, int64_t dim, int64_t classes, bool aligned
     auto take = [&](int64_t bytes) { const int64_t at = o; o += round_up(bytes, 256); return at; };
     p.thin = tiles_r * tiles_c < kSmallTiles;
     p.wide = round_up(dim, 16 / p.esz);
-    p.pad_x = !aligned_x && (dtype == 1 || p.thin);
-    p.pad_w = !aligned_w && (dtype == 1 || p.thin);
-    p.split = dtype != 1 && (!p.thin || backward);
+    p.narrow = p.thin && dtype != 1 && rows <= 32;
+    p.pad_x = !aligned_x && (dtype == 1 || p.narrow);
+    p.pad_w = !aligned_w && (dtype == 1 || p.narrow);
+    p.split = dtype != 1 && (!p.narrow || backward);
     p.split_ld = planes_bytes(dim);
     p.x_at = take(p.pad_x ? rows * p.wide * p.esz : 0);
     p.w_at = take(p.pad_w ? classes * p.wide * p.esz : 0);
     p.xs_at = take(p.split ? rows * p.split_ld : 0);
     p.ws_at = take(p.split ? classes * p.split_ld : 0);
     if (p.thin) {
-        const int64_t steps = ceil_div(p.wide * p.esz, kStepBytes), small = ceil_div(rows, 32) * ceil_div(classes, 32);
-        const int64_t waves = std::max<int64_t>(4, std::min<int64_t>(kWantWaves / small, steps));
-        p.thin_cuts = (int)std::max<int64_t>(1, waves / 4);
-        p.thin_steps = (int)ceil_div(steps, p.thin_cuts * 4);
-        p.thin_cuts = (int)ceil_div(steps, p.thin_steps * 4);
+        if (p.narrow) {
+            const int64_t steps = ceil_div(p.wide * p.esz, kStepBytes);
+            const int64_t waves = std::max<int64_t>(4, std::min<int64_t>(kWantWaves / ceil_div(classes, 32), steps));
+            p.thin_cuts = (int)std::max<int64_t>(1, waves / 4);
+            p.thin_steps = (int)ceil_div(steps, p.thin_cuts * 4);
+            p.thin_cuts = (int)ceil_div(steps, p.thin_steps * 4);
+        } else {
+            p.thin_z = lay_out(rows, classes, dim, true);
+            p.thin_cuts = (int)p.thin_z.cuts;
+        }
         p.z_ld = round_up(classes, 32);
         const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(ceil_div(classes, kThinPart), kWantBlocks / rows));
         p.thin_part = round_up(ceil_div(classes, parts), 4);
@@ -822,7 +826,7 @@ template <typename T> Matrix padded(const void* src, int64_t ld, int64_t rows, i
 struct Inputs { Matrix x, w; Operand xo, wo; };
 template <typename T> Inputs inputs_of(const ClassifierCall& c, const Plan& p, char* work, hipStream_t st) {
     Inputs in = {};
-    if (sizeof(T) == 2 || p.thin) {
+    if (sizeof(T) == 2 || p.narrow) {
         in.x = padded<T>(c.x, c.ldx, c.rows, c.dim, p, p.pad_x, p.x_at, work, st);
         in.w = padded<T>(c.w, c.ldw, c.classes, c.dim, p, p.pad_w, p.w_at, work, st);
     }
@@ -844,22 +848,6 @@ template <typename T> Inputs inputs_of(const ClassifierCall& c, const Plan& p, c
 // the same memory with its lines the reduction: `rows` outputs (up to whole pieces) by `k` lines
 Operand across(const Operand& o, int64_t rows, int64_t k) { return Operand{o.p, o.ld, rows, k, o.stored}; }
 
-template <typename T> ThinRows thin_forward(const Matrix& x, const Matrix& w, const float* bias, const RowFacts& facts, const Plan& p, char* work, hipStream_t st) {
-    ThinArgs t = {};
-    t.w = w;
-    t.x = x;
-    t.row_bytes = p.wide * p.esz;
-    t.steps = (int)ceil_div(t.row_bytes, kStepBytes);
-    t.steps_per_wave = p.thin_steps;
-    t.tiles_m = (int)ceil_div(w.rows, 32);
-    t.tiles_n = (int)ceil_div(x.rows, 32);
-    t.z = (float*)(work + p.z_at);
-    t.z_ld = p.z_ld;
-    ProfScope ps("classifier_thin_logits", 2.0 * x.rows * w.rows * p.wide, (double)(x.rows + w.rows) * p.wide * p.esz, st);
-    hipLaunchKernelGGL((thin_logits_kernel<T>), dim3((unsigned)(t.tiles_m * t.tiles_n * p.thin_cuts)), dim3(256), 0, st, t);
-    return ThinRows{t.z, p.z_ld, x.rows, w.rows, p.thin_cuts, bias, facts};
-}
-
 // a by b, `cut` elements of the reduction to a block, on tiles as laid out
 template <Want WANT, int PA, int PB, bool A_ALONG, bool B_ALONG, typename OUT> void launch_gemm(GemmArgs& g, int64_t cut, bool big, hipStream_t st) {
     constexpr int KS = Steps<PA, PB>::KS;
@@ -875,6 +863,33 @@ template <Want WANT, int PA, int PB, bool A_ALONG, bool B_ALONG, typename OUT> v
 }
 constexpr int64_t kWhole = 1ll << 30;          // no cuts
 
+template <typename T> ThinRows thin_forward(const Inputs& in, const float* bias, const RowFacts& facts, const Plan& p, const ClassifierCall& c, char* work, hipStream_t st) {
+    constexpr int P = sizeof(T) == 2 ? 1 : 3;
+    float* const z = (float*)(work + p.z_at);
+    ProfScope ps("classifier_thin_logits", 2.0 * c.rows * c.classes * c.dim, (double)(c.rows + c.classes) * c.dim * p.esz, st);
+    if (p.narrow) {
+        ThinArgs t = {};
+        t.w = in.w;
+        t.x = in.x;
+        t.row_bytes = p.wide * p.esz;
+        t.steps = (int)ceil_div(t.row_bytes, kStepBytes);
+        t.steps_per_wave = p.thin_steps;
+        t.tiles = (int)ceil_div(c.classes, 32);
+        t.z = z;
+        t.z_ld = p.z_ld;
+        hipLaunchKernelGGL(thin_logits_kernel, dim3((unsigned)(t.tiles * p.thin_cuts)), dim3(256), 0, st, t);
+    } else {
+        GemmArgs g = {};
+        g.a = in.xo;
+        g.b = in.wo;
+        g.out = z;
+        g.out_ld = p.z_ld;
+        g.out_cut = c.rows * p.z_ld;
+        launch_gemm<PRODUCT, P, P, true, true, float>(g, p.thin_z.per_cut, p.thin_z.big, st);
+    }
+    return ThinRows{z, p.z_ld, c.rows, c.classes, p.thin_cuts, bias, facts};
+}
+
 template <typename T> void forward(const ClassifierCall& c, const ClassifierOut& out, hipStream_t st) {
     constexpr int P = sizeof(T) == 2 ? 1 : 3;
     const Plan p = plan_of(c.dtype, c.rows, c.dim, c.classes, lies_aligned(c.x, c.ldx, c.dim, sizeof(T)), lies_aligned(c.w, c.ldw, c.dim, sizeof(T)), false);
@@ -887,7 +902,7 @@ template <typename T> void forward(const ClassifierCall& c, const ClassifierOut&
     float* const target_z = (float*)(work + p.target_at);
     int64_t tiles = p.z_tiles;
     if (p.thin) {
-        const ThinRows z = thin_forward<T>(in.x, in.w, c.bias, facts, p, work, st);
+        const ThinRows z = thin_forward<T>(in, c.bias, facts, p, c, work, st);
         ProfScope ps("classifier_thin_sums", 0.0, 4.0 * p.thin_cuts * c.rows * c.classes, st);
         hipLaunchKernelGGL(thin_sums_kernel, dim3((unsigned)(c.rows * p.thin_parts)), dim3(256), 0, st, z, p.thin_parts, p.thin_part, sums, target_z, res);
         tiles = p.thin_parts;
@@ -929,7 +944,7 @@ template <typename T> void backward(const ClassifierCall& c, const ClassifierGra
         wq.rows = n;
         float* const db = d.dbias == nullptr ? nullptr : p.z_tiles > 1 ? (float*)(work + p.db_at) : d.dbias + from;
         if (p.thin) {
-            const ThinRows z = thin_forward<T>(in.x, in.w, c.bias, facts, p, work, st);
+            const ThinRows z = thin_forward<T>(in, c.bias, facts, p, c, work, st);
             {
                 ProfScope ps("classifier_thin_grads", 0.0, (4.0 * p.thin_cuts + 6.0) * c.rows * c.classes, st);
                 hipLaunchKernelGGL(thin_grads_kernel, dim3((unsigned)(c.rows * ceil_div(cols / 4, 256))), dim3(256), 0, st, z, dz, p.dz_ld, (int)cols);
