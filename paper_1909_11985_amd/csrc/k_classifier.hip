@@ -198,14 +198,19 @@ __device__ __forceinline__ void tile_of(const GemmArgs& g, int& tm, int& tn, int
 // instructions, 128x64 read 6 KB for 8; what the larger tile needs is enough of them for the chip.
 struct Shape128 { static constexpr int WM = 2, WN = 2, TM = 2, TN = 2, SIDE = 128; };
 struct Shape256 { static constexpr int WM = 2, WN = 4, TM = 4, TN = 2, SIDE = 256; };
-// Elements of a reduction step and steps in LDS at a time, for PA and PB planes: 32 KB (256x256 tiles: 64 at most) to a step, and
-// as many as fit, so that loads of the steps to come are always in flight.
-template <int PA, int PB> struct Steps { static constexpr int KS = PA + PB <= 3 ? 32 : 16, STAGES = PA + PB == 2 || PA + PB == 4 ? 4 : 3; };
+// Elements of a reduction step and steps in LDS at a time, for PA and PB planes: long steps, because a step's part of a line
+// is asked for at once and parts of 32 bytes take the caches twice as long as parts of 64 (dw of 4,096 x 1,024 x 32,768 bf16:
+// 880 us with planes in groups of 16 elements, 594 with whole lines), and as many as fit, so that loads of the steps
+// to come are always in flight.
+template <int PA, int PB, int SIDE> struct Steps {
+    static constexpr int KS = PA + PB == 4 || (PA + PB == 6 && SIDE == 256) ? 16 : 32;
+    static constexpr int STAGES = PA + PB == 2 || PA + PB == 4 ? 4 : 3;
+};
 
 template <Want WANT, int PA, int PB, bool A_ALONG, bool B_ALONG, typename OUT, typename SHAPE>
 __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmArgs g) {
     constexpr int WM = SHAPE::WM, WN = SHAPE::WN, TM = SHAPE::TM, TN = SHAPE::TN, THREADS = WM * WN * 64, SIDE = SHAPE::SIDE;
-    constexpr int KS = Steps<PA, PB>::KS, STAGES = Steps<PA, PB>::STAGES;
+    constexpr int KS = Steps<PA, PB, SIDE>::KS, STAGES = Steps<PA, PB, SIDE>::STAGES;
     typedef Tile<A_ALONG, SIDE, PA, KS, THREADS> TA;
     typedef Tile<B_ALONG, SIDE, PB, KS, THREADS> TB;
     constexpr int STAGE = TA::BYTES + TB::BYTES;
@@ -850,8 +855,7 @@ Operand across(const Operand& o, int64_t rows, int64_t k) { return Operand{o.p, 
 
 // a by b, `cut` elements of the reduction to a block, on tiles as laid out
 template <Want WANT, int PA, int PB, bool A_ALONG, bool B_ALONG, typename OUT> void launch_gemm(GemmArgs& g, int64_t cut, bool big, hipStream_t st) {
-    constexpr int KS = Steps<PA, PB>::KS;
-    const int64_t side = big ? kBigTile : kTile;
+    const int64_t side = big ? kBigTile : kTile, KS = big ? Steps<PA, PB, 256>::KS : Steps<PA, PB, 128>::KS;
     g.steps = (int)ceil_div(g.a.k, KS);
     g.steps_per_cut = (int)std::min<int64_t>(g.steps, cut / KS);       // (a cut is a multiple of 64)
     g.tiles_m = (int)ceil_div(g.a.rows, side);
