@@ -440,46 +440,71 @@ __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmAr
 
 // ---- few tiles ----------------------------------------------------------------------------------------------------------
 // Where z has too few tiles to fill the chip its reduction is cut as well and its float32 parts are stored: [cut][rows][z_ld].
-// They come from gemm_kernel, or, of up to 32 float32 rows (which would not repay the copies that it needs), from this one: a
-// wave has 32 rows of w and its part of the reduction, on float32 matrix instructions, fragments straight from memory.
+// They come from gemm_kernel, or, of up to 32 rows (which would waste most of a tile, and not repay the copies that float32 or
+// odd rows need there), from this one: a wave has 32 rows of w and its part of the reduction, fragments straight from memory as
+// they lie.  What bounds it is reading w once.
 constexpr int kStepBytes = 128;        // of a reduction step
-struct Matrix { const char* p; int64_t ld, rows; };        // ld in bytes; 16-byte aligned
+struct Matrix { const char* p; int64_t ld, rows; };        // ld in bytes
 struct ThinArgs {
     Matrix w, x;
-    int64_t row_bytes;         // whole 16 bytes
+    int64_t row_bytes;
     int steps, steps_per_wave, tiles;
     float* z;
     int64_t z_ld;
 };
-__global__ __launch_bounds__(256) void thin_logits_kernel(ThinArgs g) {
+template <typename T> __device__ __forceinline__ uint4 load_piece_of_row(const char* row, int64_t at, int64_t row_bytes) {
+    constexpr int ESZ = (int)sizeof(T);
+    if (at + 16 <= row_bytes) return load_loose(reinterpret_cast<const T*>(row + at)).u;
+    Vec16<T> v;
+#pragma unroll
+    for (int e = 0; e < 16 / ESZ; ++e) v.e[e] = at + (e + 1) * ESZ <= row_bytes ? reinterpret_cast<const T*>(row + at)[e] : (T)0;
+    return v.u;
+}
+template <typename T> __global__ __launch_bounds__(256) void thin_logits_kernel(ThinArgs g) {
     __shared__ float part[4][16][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int tm = (int)(blockIdx.x % (unsigned)g.tiles), cut = (int)(blockIdx.x / (unsigned)g.tiles);
     const int64_t m = min((int64_t)tm * 32 + (lane & 31), g.w.rows - 1), n = min((int64_t)(lane & 31), g.x.rows - 1);
     const int first = (cut * 4 + wave) * g.steps_per_wave, last = min(first + g.steps_per_wave, g.steps);
-    int64_t at = (int64_t)first * kStepBytes + 16 * (lane >> 5);
     const char* const a = g.w.p + m * g.w.ld;
     const char* const b = g.x.p + n * g.x.ld;
     floatx16 acc;
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[e] = 0.f;
-    for (int s = first; s < last; ++s, at += kStepBytes) {
+    auto contract = [&](const uint4 (&fa)[4], const uint4 (&fb)[4]) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if constexpr (sizeof(T) == 2) {
+                acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fa[q]), __builtin_bit_cast(bf16x8, fb[q]), acc, 0, 0, 0);
+            } else {
+                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(fa[q].x), __uint_as_float(fb[q].x), acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(fa[q].y), __uint_as_float(fb[q].y), acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(fa[q].z), __uint_as_float(fb[q].z), acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(fa[q].w), __uint_as_float(fb[q].w), acc, 0, 0, 0);
+            }
+        }
+    };
+    const int whole = min(last, (int)(g.row_bytes / kStepBytes));
+    int64_t at = (int64_t)first * kStepBytes + 16 * (lane >> 5);
+    int s = first;
+#pragma unroll 2
+    for (; s < whole; ++s, at += kStepBytes) {
         uint4 fa[4], fb[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const bool in = at + 32 * q < g.row_bytes;
-            const int64_t from = in ? at + 32 * q : 0;      // (row starts are always there)
-            fa[q] = *reinterpret_cast<const uint4*>(a + from);
-            fb[q] = *reinterpret_cast<const uint4*>(b + from);
-            if (!in) fa[q] = fb[q] = make_uint4(0, 0, 0, 0);
+            fa[q] = load_loose(reinterpret_cast<const T*>(a + at + 32 * q)).u;
+            fb[q] = load_loose(reinterpret_cast<const T*>(b + at + 32 * q)).u;
         }
+        contract(fa, fb);
+    }
+    if (s < last) {                    // the end of the rows
+        uint4 fa[4], fb[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(fa[q].x), __uint_as_float(fb[q].x), acc, 0, 0, 0);
-            acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(fa[q].y), __uint_as_float(fb[q].y), acc, 0, 0, 0);
-            acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(fa[q].z), __uint_as_float(fb[q].z), acc, 0, 0, 0);
-            acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(fa[q].w), __uint_as_float(fb[q].w), acc, 0, 0, 0);
+            fa[q] = load_piece_of_row<T>(a, at + 32 * q, g.row_bytes);
+            fb[q] = load_piece_of_row<T>(b, at + 32 * q, g.row_bytes);
         }
+        contract(fa, fb);
     }
 #pragma unroll
     for (int e = 0; e < 16; ++e) part[wave][e][lane] = acc[e];
@@ -648,19 +673,18 @@ __global__ __launch_bounds__(256) void sum_slots_kernel(const float* __restrict_
     out[r * ld + (i - r * cols)] = Elem<OUT>::from_f32(s);
 }
 
-// rows of `cols` elements, copied to rows of `wide` (whole 16 bytes), zeros past them; a lane has 16 bytes
-template <typename T>
-__global__ __launch_bounds__(256) void pad_rows_kernel(const T* __restrict__ src, int64_t ld, int64_t cols, T* __restrict__ dst, int64_t wide, int64_t n) {
-    constexpr int VEC = Elem<T>::VEC;
+// rows of `cols` bf16 elements, copied to rows of `wide` (whole 16 bytes), zeros past them; a lane has 16 bytes
+__global__ __launch_bounds__(256) void pad_rows_kernel(const bf16_t* __restrict__ src, int64_t ld, int64_t cols, bf16_t* __restrict__ dst, int64_t wide, int64_t n) {
+    constexpr int VEC = Elem<bf16_t>::VEC;
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= n) return;
     const int64_t vecs = wide / VEC, row = i / vecs, c = (i - row * vecs) * VEC;
-    Vec16<T> v;
+    Vec16<bf16_t> v;
     if (c + VEC <= cols) {
         v = load_loose(src + row * ld + c);
     } else {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) v.e[e] = c + e < cols ? src[row * ld + c + e] : (T)0;
+        for (int e = 0; e < VEC; ++e) v.e[e] = c + e < cols ? src[row * ld + c + e] : (bf16_t)0;
     }
     store_vec(dst + row * wide + c, v);
 }
@@ -737,11 +761,10 @@ Layout lay_out(int64_t M, int64_t N, int64_t K, bool may_cut) {
 struct Plan {
     int esz;
     bool thin;
-    // x and w as thin_logits_kernel reads them, and in bf16 everything: where they lie, or copied to whole 16 bytes
-    int64_t wide;              // features up to whole 16 bytes
-    bool pad_x, pad_w;
-    // float32: x and w as three planes, for the products on tiles
-    bool split;
+    // x and w as the products on tiles read them: bf16 where they lie, or copied to whole 16 bytes; float32 copied to three planes
+    bool tiles;                // there are such products
+    int64_t wide;              // bf16: features up to whole 16 bytes
+    bool pad_x, pad_w, split;
     int64_t split_ld;          // bytes
     bool narrow;               // thin_logits_kernel
     int thin_cuts, thin_steps;         // of the reduction: cuts over blocks, steps of a wave of it
@@ -762,12 +785,13 @@ Plan plan_of(int dtype, int64_t rows, int64_t dim, int64_t classes, bool aligned
     const int64_t tiles_r = ceil_div(rows, kTile), tiles_c = ceil_div(classes, kTile);
     int64_t o = 0;
     auto take = [&](int64_t bytes) { const int64_t at = o; o += round_up(bytes, 256); return at; };
-    p.thin = tiles_r * tiles_c < kSmallTiles;
-    p.wide = round_up(dim, 16 / p.esz);
-    p.narrow = p.thin && dtype != 1 && rows <= 32;
-    p.pad_x = !aligned_x && (dtype == 1 || p.narrow);
-    p.pad_w = !aligned_w && (dtype == 1 || p.narrow);
-    p.split = dtype != 1 && (!p.narrow || backward);
+    p.narrow = rows <= 32 && classes <= kMostAtOnce;
+    p.thin = p.narrow || tiles_r * tiles_c < kSmallTiles;
+    p.tiles = !p.narrow || backward;
+    p.wide = round_up(dim, 8);
+    p.pad_x = p.tiles && dtype == 1 && !aligned_x;
+    p.pad_w = p.tiles && dtype == 1 && !aligned_w;
+    p.split = p.tiles && dtype != 1;
     p.split_ld = planes_bytes(dim);
     p.x_at = take(p.pad_x ? rows * p.wide * p.esz : 0);
     p.w_at = take(p.pad_w ? classes * p.wide * p.esz : 0);
@@ -775,7 +799,7 @@ Plan plan_of(int dtype, int64_t rows, int64_t dim, int64_t classes, bool aligned
     p.ws_at = take(p.split ? classes * p.split_ld : 0);
     if (p.thin) {
         if (p.narrow) {
-            const int64_t steps = ceil_div(p.wide * p.esz, kStepBytes);
+            const int64_t steps = ceil_div(dim * p.esz, kStepBytes);
             const int64_t waves = std::max<int64_t>(4, std::min<int64_t>(kWantWaves / ceil_div(classes, 32), steps));
             p.thin_cuts = (int)std::max<int64_t>(1, waves / 4);
             p.thin_steps = (int)ceil_div(steps, p.thin_cuts * 4);
@@ -819,35 +843,26 @@ bool lies_aligned(const void* p, int64_t ld, int64_t dim, int esz) {
     return (uintptr_t)p % 16 == 0 && ld * esz % 16 == 0 && dim * esz % 16 == 0 && ld * esz <= (1 << 23);
 }
 
-// x or w as Plan says thin_logits_kernel reads it
-template <typename T> Matrix padded(const void* src, int64_t ld, int64_t rows, int64_t dim, const Plan& p, bool pad, int64_t at, char* work, hipStream_t st) {
-    if (!pad) return Matrix{(const char*)src, ld * p.esz, rows};
-    const int64_t n = rows * (p.wide * p.esz / 16);
-    ProfScope ps("classifier_pad", 0.0, (double)rows * (dim + p.wide) * p.esz, st);
-    hipLaunchKernelGGL((pad_rows_kernel<T>), dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, st, (const T*)src, ld, dim, (T*)(work + at), p.wide, n);
-    return Matrix{work + at, p.wide * p.esz, rows};
-}
-// x and w as operands whose reduction lies along them, in bf16 from their matrices
-struct Inputs { Matrix x, w; Operand xo, wo; };
+// x and w as operands whose reduction lies along them
+struct Inputs { Operand x, w; };
 template <typename T> Inputs inputs_of(const ClassifierCall& c, const Plan& p, char* work, hipStream_t st) {
-    Inputs in = {};
-    if (sizeof(T) == 2 || p.narrow) {
-        in.x = padded<T>(c.x, c.ldx, c.rows, c.dim, p, p.pad_x, p.x_at, work, st);
-        in.w = padded<T>(c.w, c.ldw, c.classes, c.dim, p, p.pad_w, p.w_at, work, st);
-    }
-    if (sizeof(T) == 2) {
-        in.xo = Operand{in.x.p, in.x.ld, c.rows, p.wide, 1};
-        in.wo = Operand{in.w.p, in.w.ld, c.classes, p.wide, 1};
-    } else if (p.split) {
-        auto split = [&](const void* src, int64_t ld, int64_t rows, int64_t at) {
+    auto operand = [&](const void* src, int64_t ld, int64_t rows, bool pad, int64_t pad_at, int64_t split_at) {
+        if (!p.tiles) return Operand{};
+        if (sizeof(T) == 4) {
             const int64_t n = rows * (p.split_ld / kGroupBytes * (kGroup / 4));
             ProfScope ps("classifier_split", 0.0, (4.0 * c.dim + p.split_ld) * rows, st);
-            hipLaunchKernelGGL(split_rows_kernel, dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, st, (const float*)src, ld, c.dim, work + at, p.split_ld, n);
-            return Operand{work + at, p.split_ld, rows, round_up(c.dim, 16), 3};
-        };
-        in.xo = split(c.x, c.ldx, c.rows, p.xs_at);
-        in.wo = split(c.w, c.ldw, c.classes, p.ws_at);
-    }
+            hipLaunchKernelGGL(split_rows_kernel, dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, st, (const float*)src, ld, c.dim, work + split_at, p.split_ld, n);
+            return Operand{work + split_at, p.split_ld, rows, round_up(c.dim, 16), 3};
+        }
+        if (!pad) return Operand{(const char*)src, ld * 2, rows, p.wide, 1};
+        const int64_t n = rows * (p.wide / 8);
+        ProfScope ps("classifier_pad", 0.0, 2.0 * rows * (c.dim + p.wide), st);
+        hipLaunchKernelGGL(pad_rows_kernel, dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, st, (const bf16_t*)src, ld, c.dim, (bf16_t*)(work + pad_at), p.wide, n);
+        return Operand{work + pad_at, p.wide * 2, rows, p.wide, 1};
+    };
+    Inputs in;
+    in.x = operand(c.x, c.ldx, c.rows, p.pad_x, p.x_at, p.xs_at);
+    in.w = operand(c.w, c.ldw, c.classes, p.pad_w, p.w_at, p.ws_at);
     return in;
 }
 // the same memory with its lines the reduction: `rows` outputs (up to whole pieces) by `k` lines
@@ -873,19 +888,19 @@ template <typename T> ThinRows thin_forward(const Inputs& in, const float* bias,
     ProfScope ps("classifier_thin_logits", 2.0 * c.rows * c.classes * c.dim, (double)(c.rows + c.classes) * c.dim * p.esz, st);
     if (p.narrow) {
         ThinArgs t = {};
-        t.w = in.w;
-        t.x = in.x;
-        t.row_bytes = p.wide * p.esz;
+        t.w = Matrix{(const char*)c.w, c.ldw * p.esz, c.classes};
+        t.x = Matrix{(const char*)c.x, c.ldx * p.esz, c.rows};
+        t.row_bytes = c.dim * p.esz;
         t.steps = (int)ceil_div(t.row_bytes, kStepBytes);
         t.steps_per_wave = p.thin_steps;
         t.tiles = (int)ceil_div(c.classes, 32);
         t.z = z;
         t.z_ld = p.z_ld;
-        hipLaunchKernelGGL(thin_logits_kernel, dim3((unsigned)(t.tiles * p.thin_cuts)), dim3(256), 0, st, t);
+        hipLaunchKernelGGL((thin_logits_kernel<T>), dim3((unsigned)(t.tiles * p.thin_cuts)), dim3(256), 0, st, t);
     } else {
         GemmArgs g = {};
-        g.a = in.xo;
-        g.b = in.wo;
+        g.a = in.x;
+        g.b = in.w;
         g.out = z;
         g.out_ld = p.z_ld;
         g.out_cut = c.rows * p.z_ld;
@@ -913,8 +928,8 @@ template <typename T> void forward(const ClassifierCall& c, const ClassifierOut&
         if (tiles == 1) return;
     } else {
         GemmArgs g = {};
-        g.a = in.wo;
-        g.b = in.xo;
+        g.a = in.w;
+        g.b = in.x;
         g.bias = c.bias;
         g.classes = c.classes;
         g.facts = facts;
@@ -943,7 +958,7 @@ template <typename T> void backward(const ClassifierCall& c, const ClassifierGra
     const int64_t slots = p.chunks * p.dx.cuts;
     for (int64_t q = 0; q < p.chunks; ++q) {
         const int64_t from = q * p.chunk, n = std::min(p.chunk, c.classes - from), cols = round_up(n, 16);
-        Operand wq = in.wo;
+        Operand wq = in.w;
         wq.p += from * wq.ld;
         wq.rows = n;
         float* const db = d.dbias == nullptr ? nullptr : p.z_tiles > 1 ? (float*)(work + p.db_at) : d.dbias + from;
@@ -960,7 +975,7 @@ template <typename T> void backward(const ClassifierCall& c, const ClassifierGra
         } else {
             GemmArgs g = {};
             g.a = wq;
-            g.b = in.xo;
+            g.b = in.x;
             g.bias = c.bias;
             g.first_class = from;
             g.classes = from + n;
@@ -997,7 +1012,7 @@ template <typename T> void backward(const ClassifierCall& c, const ClassifierGra
         {
             GemmArgs g = {};
             g.a = Operand{dz, p.dz_ld, n, c.rows, 3};
-            g.b = across(in.xo, c.dim, c.rows);
+            g.b = across(in.x, c.dim, c.rows);
             const bool cut = p.dw.cuts > 1;
             g.out = cut ? (float*)(work + p.dw_at) : d.dw + from * d.lddw;
             g.out_ld = cut ? c.dim : d.lddw;
