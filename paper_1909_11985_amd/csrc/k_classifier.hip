@@ -636,25 +636,32 @@ __global__ __launch_bounds__(256) void thin_bias_kernel(const char* dz, int64_t 
 }
 
 // ---- joins --------------------------------------------------------------------------------------------------------------
-// The sums of a row's tiles [tile][rows]: 32 rows by 8 groups of tiles to a block.
+// The sums of a row's tiles [tile][rows]: a block has ROWS rows, the rest of its threads share their tiles.  32 rows read half a
+// kilobyte at a time; where that leaves few blocks, four.
+template <int ROWS>
 __global__ __launch_bounds__(256) void classifier_join_kernel(const float4* __restrict__ sums, int64_t tiles, int64_t rows, const int32_t* targets,
                                                               int64_t classes, const float* target_z, RowResults out) {
-    __shared__ float4 part[8][32];
-    const int r = threadIdx.x & 31, group = threadIdx.x >> 5;
-    const int64_t row = (int64_t)blockIdx.x * 32 + r;
+    __shared__ float4 part[4][ROWS];
+    const int r = threadIdx.x % ROWS, lane = threadIdx.x & 63;
+    const int64_t row = (int64_t)blockIdx.x * ROWS + r;
     SoftmaxSums s;
-    if (row < rows)
-        for (int64_t t = group; t < tiles; t += 8) {
+    if (row < rows) {
+#pragma unroll 4
+        for (int64_t t = threadIdx.x / ROWS; t < tiles; t += 256 / ROWS) {
             const float4 p = sums[t * rows + row];
             SoftmaxSums o;
             o.m = p.x; o.s = p.y; o.t = p.z;
             softmax_join(s, o);
         }
-    part[group][r] = make_float4(s.m, s.s, s.t, 0.f);
+    }
+#pragma unroll
+    for (int o = ROWS; o < 64; o <<= 1) softmax_join(s, softmax_shuffle(s, o));
+    if (lane < ROWS) part[threadIdx.x >> 6][r] = make_float4(s.m, s.s, s.t, 0.f);
     __syncthreads();
-    if (group != 0 || row >= rows) return;
-    for (int q = 1; q < 8; ++q) {
-        const float4 p = part[q][r];
+    if (threadIdx.x >= ROWS || row >= rows) return;
+#pragma unroll
+    for (int w = 1; w < 4; ++w) {
+        const float4 p = part[w][r];
         SoftmaxSums o;
         o.m = p.x; o.s = p.y; o.t = p.z;
         softmax_join(s, o);
@@ -735,6 +742,7 @@ constexpr int64_t kMostAtOnce = 1 << 20;       // classes of it: offsets in a ti
 constexpr int64_t kWantBlocks = 512;           // two blocks of 128x128 per CU
 constexpr int64_t kChip = 256;                 // CUs: one block of 256x256 each
 constexpr int64_t kWantWaves = 2048;
+constexpr int64_t kFewRows = 1024;            // a block of classifier_join_kernel has four of them
 constexpr int64_t kThinPart = 4096;            // classes of a part of a row, at least, where rows are few
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -785,7 +793,9 @@ Plan plan_of(int dtype, int64_t rows, int64_t dim, int64_t classes, bool aligned
     const int64_t tiles_r = ceil_div(rows, kTile), tiles_c = ceil_div(classes, kTile);
     int64_t o = 0;
     auto take = [&](int64_t bytes) { const int64_t at = o; o += round_up(bytes, 256); return at; };
-    p.narrow = rows <= 32 && classes <= kMostAtOnce;
+    // (tiles of 128 rows read w faster where they need no copies of it: 32 rows of 4,096 bf16 features, 50,000 classes 104 us on
+    // tiles, 155 by rows; 4 rows, 128,000 classes 200 against 241)
+    p.narrow = rows <= 32 && classes <= kMostAtOnce && (dtype != 1 || !aligned_x || !aligned_w || tiles_r * tiles_c < kSmallTiles);
     p.thin = p.narrow || tiles_r * tiles_c < kSmallTiles;
     p.tiles = !p.narrow || backward;
     p.wide = round_up(dim, 8);
@@ -939,7 +949,10 @@ template <typename T> void forward(const ClassifierCall& c, const ClassifierOut&
         launch_gemm<SUMS, P, P, true, true, float>(g, kWhole, p.z.big, st);
     }
     ProfScope ps("classifier_join", 0.0, 16.0 * tiles * c.rows, st);
-    hipLaunchKernelGGL(classifier_join_kernel, dim3((unsigned)ceil_div(c.rows, 32)), dim3(256), 0, st, sums, tiles, c.rows, c.targets, c.classes, target_z, res);
+    if (c.rows <= kFewRows)
+        hipLaunchKernelGGL((classifier_join_kernel<4>), dim3((unsigned)ceil_div(c.rows, 4)), dim3(256), 0, st, sums, tiles, c.rows, c.targets, c.classes, target_z, res);
+    else
+        hipLaunchKernelGGL((classifier_join_kernel<32>), dim3((unsigned)ceil_div(c.rows, 32)), dim3(256), 0, st, sums, tiles, c.rows, c.targets, c.classes, target_z, res);
 }
 
 template <typename OUT> void sum_slots(const float* part, int64_t slots, int64_t rows, int64_t cols, OUT* out, int64_t ld, hipStream_t st) {
@@ -1030,8 +1043,15 @@ template <typename T> void backward(const ClassifierCall& c, const ClassifierGra
 
 size_t classifier_work_bytes(const ClassifierCall& c, bool backward) {
     const int esz = c.dtype == 1 ? 2 : 4;
-    const bool ax = c.x == nullptr ? false : lies_aligned(c.x, c.ldx, c.dim, esz), aw = c.w == nullptr ? false : lies_aligned(c.w, c.ldw, c.dim, esz);
-    return (size_t)plan_of(c.dtype, c.rows, c.dim, c.classes, ax, aw, backward).bytes;
+    // (however they lie: the most of both ways)
+    int64_t most = 0;
+    for (int way = 0; way < 4; ++way) {
+        const bool ax = (way & 1) != 0, aw = (way & 2) != 0;
+        if (c.x != nullptr && ax != lies_aligned(c.x, c.ldx, c.dim, esz)) continue;
+        if (c.w != nullptr && aw != lies_aligned(c.w, c.ldw, c.dim, esz)) continue;
+        most = std::max(most, plan_of(c.dtype, c.rows, c.dim, c.classes, ax, aw, backward).bytes);
+    }
+    return (size_t)most;
 }
 
 void launch_classifier(const ClassifierCall& c, const ClassifierOut& out, hipStream_t st) {

@@ -151,4 +151,8 @@ def test_classifier_workspace_grows_with_what_it_holds(E):
         for classes in (1, 100, 5000, 100001):
             for dim in (1, 64, 4096):
                 for dtype in (0, 1):
-                    assert need(None, 0, None, 0, rows, dim, classes, 0, dtype) > 0 and need(None, 0, None, 0, rows, dim, classes, 1, dtype) > 0
+                    for backward in (0, 1):
+                        any_way = need(None, 0, None, 0, rows, dim, classes, backward, dtype)
+                        ways = [need(SOME + a, dim + b, SOME + c, dim + d, rows, dim, classes, backward, dtype)
+                                for a in (0, 4) for b in (0, 1) for c in (0, 4) for d in (0, 1)]
+                        assert 0 < max(ways) <= any_way
