@@ -461,7 +461,7 @@ int32_t edl_dropout(int32_t dtype, const void* dev_x, int64_t ldx, void* dev_y, 
  * NaN (the alternatives' numbers stay classes; NaN ranks as -inf).  Sums are float32, whatever dtype is.
  * dev_work: edl_log_probs_workspace (host only) bytes, 16-byte aligned; may be NULL if that is 0.  It holds nothing between calls;
  * calls that overlap need one each.
- * EDL_EINVAL: null, misaligned or overlapping arguments, classes <= 0, k outside [0, min(64, classes)]; EDL_ENOMEM: workspace
+ * EDL_EINVAL: null or misaligned arguments, rows that overlap, classes <= 0, k outside [0, min(64, classes)]; EDL_ENOMEM: workspace
  * too small; EDL_ERANGE: rows over 2^23 or rows * ceil(classes/8) over 2^33. */
 int32_t edl_log_probs_workspace(int64_t rows, int64_t classes, int32_t k, int64_t* out_bytes);
 int32_t edl_log_probs(int32_t dtype, const void* dev_logits, int64_t ld, int64_t rows, int64_t classes, const int32_t* dev_targets, int32_t k,
@@ -485,8 +485,8 @@ int32_t edl_log_probs_backward(int32_t dtype, const void* dev_logits, int64_t ld
  * aligned, which hold nothing between calls; calls that overlap need one each.  x and w are read where they lie if address, ld and dim are multiples of
  * 16 bytes (and ld at most 2^23 bytes); else the call copies them into the workspace first, rows padded to whole 16 bytes.  Larger
  * calls, and gradients, of float32 operands copy them as three bf16 numbers each, whose products are added up in float32.
- * EDL_EINVAL: null, misaligned or overlapping arguments, dim or classes <= 0; EDL_ENOMEM: workspace too small; EDL_ERANGE: rows over 2^23,
- * dim over 2^16, classes over 2^24, rows * dim over 2^31, classes * dim over 2^33, ceil(rows/128) * ceil(classes/128) over 2^23. */
+ * EDL_EINVAL: null or misaligned arguments, rows that overlap, dim or classes <= 0; EDL_ENOMEM: workspace too small; EDL_ERANGE: rows over 2^23,
+ * dim over 2^16, classes over 2^24, rows * dim over 2^29, classes * dim over 2^33, ceil(rows/128) * ceil(classes/128) over 2^23. */
 int32_t edl_classifier_workspace(int32_t dtype, const void* dev_x, int64_t ldx, const void* dev_w, int64_t ldw, int64_t rows, int64_t dim,
                                  int64_t classes, int32_t backward, int64_t* out_bytes);
 int32_t edl_classifier_log_probs(int32_t dtype, const void* dev_x, int64_t ldx, const void* dev_w, int64_t ldw, const float* dev_bias, int64_t rows,
@@ -497,7 +497,8 @@ int32_t edl_classifier_log_probs(int32_t dtype, const void* dev_x, int64_t ldx, 
  * with dz as in edl_log_probs_backward, dx = dz w in dtype, dw = dz^T x and dbias = sum of dz over the rows in float32 (what
  * edl_average_update and edl_adam_update take; dev_dbias may be NULL).  The logits are formed again, a piece of the classes at a
  * time, and dz is stored for such a piece (at most 1 GiB of workspace, or 128 classes) as a sum of three bf16 numbers, so that dw and
- * dbias are float32 results.  All outputs are written, not added to; of no rows, dw and dbias are zeros.  Arguments and errors as
+ * dbias are float32 results.  All outputs are written, not added to, and must not
+ * overlap the inputs (the same address is refused) or each other; of no rows, dw and dbias are zeros.  Arguments and errors as
  * above; the workspace's size is another (backward = 1). */
 int32_t edl_classifier_log_probs_backward(int32_t dtype, const void* dev_x, int64_t ldx, const void* dev_w, int64_t ldw, const float* dev_bias,
                                           int64_t rows, int64_t dim, int64_t classes, const int32_t* dev_targets, const float* dev_lse,

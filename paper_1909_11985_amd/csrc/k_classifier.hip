@@ -669,13 +669,20 @@ __global__ __launch_bounds__(256) void classifier_join_kernel(const float4* __re
     write_results(out, targets, classes, row, s, target_z[row]);      // (without a target: not looked at)
 }
 
-// out[r][c] = sum over the slots of part[slot][r][c], in slot order
+// out[r][c] = sum over the slots of part[slot][r][c]: a block has 64 elements, four groups of threads every fourth slot each
 template <typename OUT>
 __global__ __launch_bounds__(256) void sum_slots_kernel(const float* __restrict__ part, int slots, int64_t slot, int64_t cols, int64_t n, OUT* out, int64_t ld) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= n) return;
-    float s = part[i];
-    for (int q = 1; q < slots; ++q) s += part[q * slot + i];
+    __shared__ float group[4][64];
+    const int64_t i = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
+    float s = 0.f;
+    if (i < n) {
+#pragma unroll 4
+        for (int q = threadIdx.x >> 6; q < slots; q += 4) s += part[q * slot + i];
+    }
+    group[threadIdx.x >> 6][threadIdx.x & 63] = s;
+    __syncthreads();
+    if (threadIdx.x >= 64 || i >= n) return;
+    s = (group[0][threadIdx.x] + group[1][threadIdx.x]) + (group[2][threadIdx.x] + group[3][threadIdx.x]);
     const int64_t r = i / cols;
     out[r * ld + (i - r * cols)] = Elem<OUT>::from_f32(s);
 }
@@ -958,7 +965,7 @@ template <typename T> void forward(const ClassifierCall& c, const ClassifierOut&
 template <typename OUT> void sum_slots(const float* part, int64_t slots, int64_t rows, int64_t cols, OUT* out, int64_t ld, hipStream_t st) {
     const int64_t n = rows * cols;
     ProfScope ps("classifier_sum", 0.0, 4.0 * slots * n + sizeof(OUT) * (double)n, st);
-    hipLaunchKernelGGL((sum_slots_kernel<OUT>), dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, st, part, (int)slots, n, cols, n, out, ld);
+    hipLaunchKernelGGL((sum_slots_kernel<OUT>), dim3((unsigned)ceil_div(n, 64)), dim3(256), 0, st, part, (int)slots, n, cols, n, out, ld);
 }
 
 template <typename T> void backward(const ClassifierCall& c, const ClassifierGrads& d, hipStream_t st) {

@@ -123,12 +123,18 @@ int32_t edl_log_probs_backward(int32_t dtype, const void* dev_logits, int64_t ld
 static int32_t check_classifier(int32_t dtype, int64_t rows, int64_t dim, int64_t classes) {
     if (!known_dtype(dtype)) return EDL_EINVAL;
     if (rows < 0 || dim <= 0 || classes <= 0) { set_error("rows must not be negative, dim and classes positive"); return EDL_EINVAL; }
-    if (rows > kMaxRows || dim > kMaxDim || classes > kMaxClasses || rows * dim > (1ll << 31) || classes * dim > (1ll << 33) ||
+    if (rows > kMaxRows || dim > kMaxDim || classes > kMaxClasses || rows * dim > (1ll << 29) || classes * dim > (1ll << 33) ||
         ((rows + 127) / 128) * ((classes + 127) / 128) > kMaxTiles) {
         set_error("%lld rows of %lld features for %lld classes are too many", (long long)rows, (long long)dim, (long long)classes);
         return EDL_ERANGE;
     }
     return EDL_OK;
+}
+
+// (of a single row, ld means nothing)
+static ClassifierCall classifier_call(int32_t dtype, const void* x, int64_t ldx, const void* w, int64_t ldw, const float* bias, int64_t rows, int64_t dim,
+                                      int64_t classes, const int32_t* targets, void* work) {
+    return ClassifierCall{dtype, x, rows == 1 ? dim : ldx, w, classes == 1 ? dim : ldw, bias, rows, dim, classes, targets, work};
 }
 
 static int32_t check_work(const ClassifierCall& c, bool backward, size_t work_bytes) {
@@ -143,8 +149,7 @@ int32_t edl_classifier_workspace(int32_t dtype, const void* dev_x, int64_t ldx, 
     if (!out_bytes) { set_error("null argument"); return EDL_EINVAL; }
     const int32_t rc = check_classifier(dtype, rows, dim, classes);
     if (rc) return rc;
-    ClassifierCall c = {};
-    c.dtype = dtype; c.x = dev_x; c.ldx = ldx; c.w = dev_w; c.ldw = ldw; c.rows = rows; c.dim = dim; c.classes = classes;
+    const ClassifierCall c = classifier_call(dtype, dev_x, ldx, dev_w, ldw, nullptr, rows, dim, classes, nullptr, nullptr);
     *out_bytes = rows == 0 ? 0 : (int64_t)classifier_work_bytes(c, backward != 0);
     return EDL_OK;
 }
@@ -158,7 +163,7 @@ int32_t edl_classifier_log_probs(int32_t dtype, const void* dev_x, int64_t ldx, 
     if (!rows_ok("x", dtype, dev_x, rows, dim, ldx) || !rows_ok("w", dtype, dev_w, classes, dim, ldw)) return EDL_EINVAL;
     if (!dev_entropy || !dev_lse || (dev_targets && !dev_log_prob)) { set_error("null argument"); return EDL_EINVAL; }
     if (!vectors_aligned({dev_bias, dev_targets, dev_log_prob, dev_entropy, dev_lse})) return EDL_EINVAL;
-    const ClassifierCall c = {dtype, dev_x, ldx, dev_w, ldw, dev_bias, rows, dim, classes, dev_targets, dev_work};
+    const ClassifierCall c = classifier_call(dtype, dev_x, ldx, dev_w, ldw, dev_bias, rows, dim, classes, dev_targets, dev_work);
     rc = check_work(c, false, work_bytes);
     if (rc) return rc;
     launch_classifier(c, ClassifierOut{dev_log_prob, dev_entropy, dev_lse}, (hipStream_t)hip_stream);
@@ -178,7 +183,11 @@ int32_t edl_classifier_log_probs_backward(int32_t dtype, const void* dev_x, int6
         if (!dev_lse || (dev_dentropy && !dev_entropy) || (dev_dlog_prob && !dev_targets)) { set_error("null argument"); return EDL_EINVAL; }
     }
     if (!vectors_aligned({dev_bias, dev_targets, dev_lse, dev_entropy, dev_dlog_prob, dev_dentropy, dev_dbias})) return EDL_EINVAL;
-    const ClassifierCall c = {dtype, dev_x, ldx, dev_w, ldw, dev_bias, rows, dim, classes, dev_targets, dev_work};
+    if (rows > 0 && (dev_dx == dev_x || dev_dx == dev_w || (const void*)dev_dw == dev_w || (const void*)dev_dw == dev_x)) {
+        set_error("gradients cannot take the place of what they are computed from");
+        return EDL_EINVAL;
+    }
+    const ClassifierCall c = classifier_call(dtype, dev_x, ldx, dev_w, ldw, dev_bias, rows, dim, classes, dev_targets, dev_work);
     if (rows > 0) {
         rc = check_work(c, true, work_bytes);
         if (rc) return rc;

@@ -110,7 +110,7 @@ CLASSIFIER_BAD = [
     (dict(dtype=2), -1), (dict(x=None), -1), (dict(w=None), -1), (dict(ldx=63), -1), (dict(ldw=63), -1), (dict(rows=-1), -1), (dict(dim=0), -1),
     (dict(classes=0), -1), (dict(lse=None), -1), (dict(b=SOME + 2), -1), (dict(t=SOME + 1), -1), (dict(x=SOME + 2), -1), (dict(work=None), -1),
     (dict(work=SOME + 16), -1), (dict(bytes=16), -3), (dict(rows=2 ** 23 + 1), -4), (dict(dim=2 ** 16 + 1, ldx=2 ** 17, ldw=2 ** 17), -4),
-    (dict(classes=2 ** 24 + 1), -4), (dict(rows=2 ** 16, dim=2 ** 16, ldx=2 ** 16, ldw=2 ** 16), -4), (dict(rows=2 ** 22, classes=2 ** 24), -4),
+    (dict(classes=2 ** 24 + 1), -4), (dict(rows=2 ** 14, dim=2 ** 16, ldx=2 ** 16, ldw=2 ** 16), -4), (dict(rows=2 ** 22, classes=2 ** 24), -4),
     (dict(classes=2 ** 22, dim=2 ** 13, ldx=2 ** 13, ldw=2 ** 13), -4)]
 
 
@@ -125,9 +125,9 @@ def test_classifier_refusals(E, change, code):
 
 @pytest.mark.parametrize("change,code", CLASSIFIER_BAD + [
     (dict(t=None), -1), (dict(ent=None), -1), (dict(dx=None), -1), (dict(lddx=63), -1), (dict(dw=None), -1), (dict(lddw=63), -1), (dict(dw=SOME + 2), -1),
-    (dict(db=SOME + 1), -1), (dict(rows=0, dw=None), -1)])
+    (dict(db=SOME + 1), -1), (dict(rows=0, dw=None), -1), (dict(dx=2 * SOME), -1), (dict(dx=3 * SOME), -1), (dict(dw=3 * SOME), -1)])
 def test_classifier_backward_refusals(E, change, code):
-    a = dict(CLASSIFIER, g=SOME, h=SOME, dx=SOME, lddx=64, dw=SOME, lddw=64, db=SOME)
+    a = dict(CLASSIFIER, x=2 * SOME, w=3 * SOME, g=SOME, h=SOME, dx=4 * SOME, lddx=64, dw=5 * SOME, lddw=64, db=SOME)
     if "ldx" in change and change["ldx"] > 64:
         a.update(lddx=change["ldx"], lddw=change["ldx"])
     a.update(change)
