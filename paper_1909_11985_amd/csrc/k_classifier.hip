@@ -441,8 +441,8 @@ __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmAr
 // ---- few tiles ----------------------------------------------------------------------------------------------------------
 // Where z has too few tiles to fill the chip its reduction is cut as well and its float32 parts are stored: [cut][rows][z_ld].
 // They come from gemm_kernel, or, of up to 32 rows (which would waste most of a tile, and not repay the copies that float32 or
-// odd rows need there), from this one: a wave has 32 rows of w and its part of the reduction, fragments straight from memory as
-// they lie.  What bounds it is reading w once.
+// odd rows need there), from this one: a wave has 32 rows of w and its part of the reduction, as they lie in memory.  What bounds
+// it is reading w once: eight lanes take 128 bytes of a row, and fragments are formed through LDS of the wave's own.
 constexpr int kStepBytes = 128;        // of a reduction step
 struct Matrix { const char* p; int64_t ld, rows; };        // ld in bytes
 struct ThinArgs {
@@ -461,51 +461,65 @@ template <typename T> __device__ __forceinline__ uint4 load_piece_of_row(const c
     return v.u;
 }
 template <typename T> __global__ __launch_bounds__(256) void thin_logits_kernel(ThinArgs g) {
-    __shared__ float part[4][16][64];
+    __shared__ __attribute__((aligned(16))) char smem[4 * 2 * 32 * kStepBytes];       // a step of w's rows and of x's for each wave
+    float (*const part)[16][64] = reinterpret_cast<float (*)[16][64]>(smem);           // ... and then the waves' sums
+    static_assert(sizeof(float) * 4 * 16 * 64 <= sizeof(smem), "fits");
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int tm = (int)(blockIdx.x % (unsigned)g.tiles), cut = (int)(blockIdx.x / (unsigned)g.tiles);
-    const int64_t m = min((int64_t)tm * 32 + (lane & 31), g.w.rows - 1), n = min((int64_t)(lane & 31), g.x.rows - 1);
-    const int first = (cut * 4 + wave) * g.steps_per_wave, last = min(first + g.steps_per_wave, g.steps);
-    const char* const a = g.w.p + m * g.w.ld;
-    const char* const b = g.x.p + n * g.x.ld;
+    const int first = (cut * 4 + wave) * g.steps_per_wave, last = min(first + g.steps_per_wave, g.steps), whole = (int)(g.row_bytes / kStepBytes);
+    const char *a[4], *b[4];           // rows 8 i + lane / 8
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        a[i] = g.w.p + min((int64_t)tm * 32 + 8 * i + (lane >> 3), g.w.rows - 1) * g.w.ld;
+        b[i] = g.x.p + min((int64_t)8 * i + (lane >> 3), g.x.rows - 1) * g.x.ld;
+    }
+    char* const mine = smem + wave * (2 * 32 * kStepBytes);
+    // 16-byte piece of a row in LDS: the 16 rows whose same piece lanes ask for together lie in banks of their own
+    auto slot = [](int row, int piece) { return row * kStepBytes + (piece ^ ((row >> 1) & 7)) * 16; };
     floatx16 acc;
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[e] = 0.f;
-    auto contract = [&](const uint4 (&fa)[4], const uint4 (&fb)[4]) {
+    uint4 va[4], vb[4];
+    auto load = [&](int s) {
+        const int64_t at = (int64_t)s * kStepBytes + 16 * (lane & 7);
+        if (s < whole) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            if constexpr (sizeof(T) == 2) {
-                acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fa[q]), __builtin_bit_cast(bf16x8, fb[q]), acc, 0, 0, 0);
-            } else {
-                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(fa[q].x), __uint_as_float(fb[q].x), acc, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(fa[q].y), __uint_as_float(fb[q].y), acc, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(fa[q].z), __uint_as_float(fb[q].z), acc, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(fa[q].w), __uint_as_float(fb[q].w), acc, 0, 0, 0);
+            for (int i = 0; i < 4; ++i) va[i] = load_loose(reinterpret_cast<const T*>(a[i] + at)).u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) vb[i] = load_loose(reinterpret_cast<const T*>(b[i] + at)).u;
+        } else {                       // the end of the rows
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                va[i] = load_piece_of_row<T>(a[i], at, g.row_bytes);
+                vb[i] = load_piece_of_row<T>(b[i], at, g.row_bytes);
             }
         }
     };
-    const int whole = min(last, (int)(g.row_bytes / kStepBytes));
-    int64_t at = (int64_t)first * kStepBytes + 16 * (lane >> 5);
-    int s = first;
-#pragma unroll 2
-    for (; s < whole; ++s, at += kStepBytes) {
-        uint4 fa[4], fb[4];
+    if (first < last) load(first);
+    for (int s = first; s < last; ++s) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            *reinterpret_cast<uint4*>(mine + slot(8 * i + (lane >> 3), lane & 7)) = va[i];
+            *reinterpret_cast<uint4*>(mine + 32 * kStepBytes + slot(8 * i + (lane >> 3), lane & 7)) = vb[i];
+        }
+        wave_lds_handover();
+        if (s + 1 < last) load(s + 1);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            fa[q] = load_loose(reinterpret_cast<const T*>(a + at + 32 * q)).u;
-            fb[q] = load_loose(reinterpret_cast<const T*>(b + at + 32 * q)).u;
+            const uint4 fa = *reinterpret_cast<const uint4*>(mine + slot(lane & 31, 2 * q + (lane >> 5)));
+            const uint4 fb = *reinterpret_cast<const uint4*>(mine + 32 * kStepBytes + slot(lane & 31, 2 * q + (lane >> 5)));
+            if constexpr (sizeof(T) == 2) {
+                acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fa), __builtin_bit_cast(bf16x8, fb), acc, 0, 0, 0);
+            } else {
+                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(fa.x), __uint_as_float(fb.x), acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(fa.y), __uint_as_float(fb.y), acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(fa.z), __uint_as_float(fb.z), acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(fa.w), __uint_as_float(fb.w), acc, 0, 0, 0);
+            }
         }
-        contract(fa, fb);
+        wave_lds_handover();
     }
-    if (s < last) {                    // the end of the rows
-        uint4 fa[4], fb[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            fa[q] = load_piece_of_row<T>(a, at + 32 * q, g.row_bytes);
-            fb[q] = load_piece_of_row<T>(b, at + 32 * q, g.row_bytes);
-        }
-        contract(fa, fb);
-    }
+    __syncthreads();                   // the steps' memory is the sums' now
 #pragma unroll
     for (int e = 0; e < 16; ++e) part[wave][e][lane] = acc[e];
     __syncthreads();
