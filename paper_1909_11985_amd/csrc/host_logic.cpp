@@ -556,7 +556,7 @@ static void build_resnet50(const edl_config& c, Graph& g) {
 
 // Biased 3x3 convolutions with ReLU in five groups (2,2,3,3,3 of them for the
 // 16-layer net, 2,2,4,4,4 for the 19-layer one), a 2x2/2 max pool after each
-// group, three fully connected layers.  No batch norm, no dropout.
+// group, three fully connected layers.  No batch norm (dropout: edl_set_dropout).
 static void build_vgg16(const edl_config& c, Graph& g) {
     const int H = pick(c.H, 224), W = pick(c.W, 224), C = pick(c.C, 3), classes = pick(c.classes, 1000);
     const int base = pick(c.arch[0], 64), fc = pick(c.arch[1], 4096);

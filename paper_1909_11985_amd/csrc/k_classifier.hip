@@ -181,6 +181,7 @@ struct GemmArgs {
     // products
     void* out;                 // [cut][a.rows][out_ld]
     int64_t out_ld, out_cut;   // elements
+    bool add;                  // to what is there (float32)
 };
 
 // (tile of a's rows, of b's rows, cut).  Consecutive blocks go to the eight dies in turn; a die's blocks are made
@@ -300,12 +301,23 @@ __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmAr
             const int64_t n = n0 + (wn * TN + j) * 32 + (lane & 31);
             if (n >= g.b.rows) continue;
 #pragma unroll
-            for (int i = 0; i < TM; ++i)
+            for (int i = 0; i < TM; ++i) {
+                const int64_t top = m0 + (wm * TM + i) * 32;
+                if constexpr (sizeof(OUT) == 4) {
+                    if (g.add) {       // (rows past the last: the last one's, so that the loads do not wait for each other)
+                        float was[16];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) was[e] = out[min(top + tile_row(e, lane), g.a.rows - 1) * g.out_ld + n];
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) acc[i][j][e] += was[e];
+                    }
+                }
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const int64_t m = m0 + (wm * TM + i) * 32 + tile_row(e, lane);
+                    const int64_t m = top + tile_row(e, lane);
                     if (m < g.a.rows) out[m * g.out_ld + n] = Elem<OUT>::from_f32(acc[i][j][e]);
                 }
+            }
         }
     } else {
         // z: rows of the tile are classes, columns rows of x.  Class of element e of tile i: c0 + place(i, e).  Past the last class
@@ -874,7 +886,7 @@ Plan plan_of(int dtype, int64_t rows, int64_t dim, int64_t classes, bool aligned
         p.z_tiles = p.thin ? ceil_div(rows, kThinBiasRows) : ceil_div(rows, p.z.big ? kBigTile : kTile);
         p.dx = lay_out(rows, dim, n, true);
         p.dw = lay_out(n, dim, rows, true);
-        p.dx_at = take(p.chunks * p.dx.cuts > 1 ? p.chunks * p.dx.cuts * rows * dim * 4 : 0);
+        p.dx_at = take(p.chunks > 1 || p.dx.cuts > 1 ? p.dx.cuts * rows * dim * 4 : 0);
         p.dw_at = take(p.dw.cuts > 1 ? p.dw.cuts * n * dim * 4 : 0);
         p.db_at = take(p.z_tiles > 1 ? p.z_tiles * n * 4 : 0);
     }
@@ -1002,7 +1014,7 @@ template <typename T> void backward(const ClassifierCall& c, const ClassifierGra
     const Inputs in = inputs_of<T>(c, p, work, st);
     const RowFacts facts = {c.targets, d.lse, d.entropy, d.dlog_prob, d.dentropy};
     char* const dz = work + p.dz_at;
-    const int64_t slots = p.chunks * p.dx.cuts;
+    const bool parts_of_dx = p.chunks > 1 || p.dx.cuts > 1;
     for (int64_t q = 0; q < p.chunks; ++q) {
         const int64_t from = q * p.chunk, n = std::min(p.chunk, c.classes - from), cols = round_up(n, 16);
         Operand wq = in.w;
@@ -1042,8 +1054,9 @@ template <typename T> void backward(const ClassifierCall& c, const ClassifierGra
             g.a = Operand{dz, p.dz_ld, c.rows, cols, 3};
             g.b = across(wq, c.dim, n);
             ProfScope ps("classifier_dx", 2.0 * c.rows * n * c.dim, 6.0 * c.rows * n + (double)p.esz * (n + c.rows) * c.dim, st);
-            if (slots > 1) {
-                g.out = (float*)(work + p.dx_at) + q * p.dx.cuts * c.rows * c.dim;
+            if (parts_of_dx) {         // (later pieces of the classes are added to the first one's cuts, of which the last may have fewer)
+                g.out = (float*)(work + p.dx_at);
+                g.add = q > 0;
                 g.out_ld = c.dim;
                 g.out_cut = c.rows * c.dim;
                 launch_gemm<PRODUCT, P == 1 ? 2 : 3, P, true, false, float>(g, p.dx.per_cut, p.dx.big, st);
@@ -1053,9 +1066,7 @@ template <typename T> void backward(const ClassifierCall& c, const ClassifierGra
                 launch_gemm<PRODUCT, P == 1 ? 2 : 3, P, true, false, T>(g, kWhole, p.dx.big, st);
             }
         }
-        // (the last piece of the classes may have fewer cuts: the slots that it leaves out are not summed)
-        if (q + 1 == p.chunks && slots > 1)
-            sum_slots<T>((const float*)(work + p.dx_at), (p.chunks - 1) * p.dx.cuts + ceil_div(n, p.dx.per_cut), c.rows, c.dim, (T*)d.dx, d.lddx, st);
+        if (q + 1 == p.chunks && parts_of_dx) sum_slots<T>((const float*)(work + p.dx_at), p.dx.cuts, c.rows, c.dim, (T*)d.dx, d.lddx, st);
         {
             GemmArgs g = {};
             g.a = Operand{dz, p.dz_ld, n, c.rows, 3};

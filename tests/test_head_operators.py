@@ -1,4 +1,6 @@
 """The operators of a classifier's head on an MI355X against plain references in 64 bits.  Run with -m gpu."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -430,6 +432,37 @@ def test_classifier_backward_in_several_pieces_of_the_classes(E):
     r = E.edl_classifier_log_probs(x, w, b.cuda(), t.cuda())
     check_stats(r, want, tol, 0)
     check_classifier_grads(E, x, w, b, t, r, z, tol, torch.randn(rows, generator=gen), torch.randn(rows, generator=gen) * 0.3)
+
+
+@pytest.mark.parametrize("dtype,rows,dim,classes", [("bf16", 70001, 9, 7000), ("f32", 70001, 9, 7000), ("bf16", 9000, 300, 40003)])
+def test_classifier_backward_in_many_pieces_adds_dx_up(E, dtype, rows, dim, classes):
+    """Three pieces of the classes: dx is the sum of their parts, of which few rows have several."""
+    x, w, b, t, gen = classifier_case(33, dtype, rows, dim, classes)
+    assert rows * classes * 6 > 2 << 30
+    g = torch.randn(rows, generator=gen).cuda()
+    r = E.edl_classifier_log_probs(x, w, b.cuda(), t.cuda())
+    dx, dw, db = E.edl_classifier_log_probs_backward(x, w, b.cuda(), t.cuda(), r.lse, r.entropy, g)
+    again = E.edl_classifier_log_probs_backward(x, w, b.cuda(), t.cuda(), r.lse, r.entropy, g)
+    assert torch.equal(dx, again[0]) and torch.equal(dw, again[1]) and torch.equal(db, again[2])
+    # of some rows, in 64 bits
+    some = torch.cat([torch.arange(0, 40), torch.arange(rows - 40, rows)])
+    x64, w64 = x.cpu().double()[some], w.cpu().double()
+    z = x64 @ w64.t() + b.double()
+    p = torch.softmax(z, 1)
+    hot = torch.zeros_like(p)
+    mine = (t[some] >= 0) & (t[some] < classes)
+    hot[mine.nonzero()[:, 0], t[some][mine].long()] = 1
+    gs = torch.where(mine, g.cpu().double()[some], torch.zeros(80, dtype=torch.float64))[:, None]
+    want = (gs * (hot - p)) @ w64
+    parts = (gs.abs() * (hot + p)) @ w64.abs()              # before they cancel
+    # a probability is off by the logit's error (dim products and sums of float32 and those of log-sum-exp, a rounding each, of
+    # terms as large as |x| |w|) and a few steps of its own, and every sum of classes by a step for each of its additions
+    size = (x64.abs() @ w64.abs().t() + b.double().abs()).amax(1, keepdim=True) + math.log(classes)
+    eps = 2.0 ** -24
+    tol = parts * eps * ((dim + 40) * size + 40 + math.sqrt(classes) + 3)
+    if dtype == "bf16":
+        tol = tol + parts * 2.0 ** -16 + want.abs() * 2.0 ** -8           # (two planes of dz; the result's rounding)
+    assert bool(((dx.cpu().double()[some] - want).abs() <= tol).all())
 
 
 @pytest.mark.parametrize("rows,dim,classes,bias", [(1100, 1024, 13000, True), (1085, 1001, 13003, False)])

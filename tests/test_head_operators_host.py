@@ -136,6 +136,14 @@ def test_classifier_backward_refusals(E, change, code):
     assert rc == code and E.lib.edl_last_error()
 
 
+def test_classifier_workspace_does_not_grow_with_the_pieces_of_the_classes(E):
+    """dx is one float32 sum (of a few cuts at most), however many pieces dz comes in."""
+    n = C.c_int64()
+    for rows, dim, classes in ((65536, 4096, 131072), (65536, 4096, 32768), (8192, 512, 500000)):
+        assert E.lib.edl_classifier_workspace(1, SOME, dim, SOME, dim, rows, dim, classes, 1, C.byref(n)) == 0
+        assert n.value <= (1 << 30) + 512 * 128 * 128 * 4 + rows * dim * 4 + (1 << 26), (rows, dim, classes, n.value)
+
+
 def test_classifier_workspace_grows_with_what_it_holds(E):
     def need(x, ldx, w, ldw, rows, dim, classes, backward, dtype=1):
         n = C.c_int64()
