@@ -161,7 +161,7 @@ __device__ __forceinline__ void store_planes(char* line, int64_t c, float (&v)[4
     for (int q = 0; q < 3; ++q) *reinterpret_cast<uint2*>(p + q * 2 * kGroup) = next_bf16(v);
 }
 
-enum Want { SUMS, GRADS, PRODUCT };     // of z: sums over classes, dz; of the others: the product itself
+enum Want { SUMS, GRADS, PRODUCT, ADDED };     // of z: sums over classes, dz; of the others: the product itself, or added to what is there
 
 struct GemmArgs {
     Operand a, b;
@@ -181,7 +181,6 @@ struct GemmArgs {
     // products
     void* out;                 // [cut][a.rows][out_ld]
     int64_t out_ld, out_cut;   // elements
-    bool add;                  // to what is there (float32)
 };
 
 // (tile of a's rows, of b's rows, cut).  Consecutive blocks go to the eight dies in turn; a die's blocks are made
@@ -294,7 +293,7 @@ __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmAr
     }
     wait_loads<0>();
     __syncthreads();           // LDS is free
-    if constexpr (WANT == PRODUCT) {
+    if constexpr (WANT == PRODUCT || WANT == ADDED) {
         OUT* const out = (OUT*)g.out + cut * g.out_cut;
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
@@ -303,14 +302,13 @@ __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmAr
 #pragma unroll
             for (int i = 0; i < TM; ++i) {
                 const int64_t top = m0 + (wm * TM + i) * 32;
-                if constexpr (sizeof(OUT) == 4) {
-                    if (g.add) {       // (rows past the last: the last one's, so that the loads do not wait for each other)
-                        float was[16];
+                if constexpr (WANT == ADDED) {         // (rows past the last: the last one's, so that the loads do not wait for each other)
+                    static_assert(sizeof(OUT) == 4, "sums are float32");
+                    float was[16];
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) was[e] = out[min(top + tile_row(e, lane), g.a.rows - 1) * g.out_ld + n];
+                    for (int e = 0; e < 16; ++e) was[e] = out[min(top + tile_row(e, lane), g.a.rows - 1) * g.out_ld + n];
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) acc[i][j][e] += was[e];
-                    }
+                    for (int e = 0; e < 16; ++e) acc[i][j][e] += was[e];
                 }
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
@@ -784,8 +782,9 @@ constexpr int64_t kSmallTiles = 192;           // z of fewer 128x128 tiles is fo
 constexpr int64_t kDzBytes = 1024 * kMiB;      // of dz at a time
 constexpr int64_t kZeroAtOnce = 1ll << 30;     // elements of dw that one launch clears where there are no rows
 constexpr int64_t kMostAtOnce = 1 << 20;       // classes of it: offsets in a tile of dz are counted in 31 bits
-constexpr int64_t kWantBlocks = 512;           // two blocks of 128x128 per CU
-constexpr int64_t kChip = 256;                 // CUs: one block of 256x256 each
+constexpr int64_t kWantBlocks = 512;           // of thin_sums_kernel
+constexpr int64_t kChip = 256;                 // CUs: a block of a product each
+constexpr int64_t kLeastOfZ = 256, kLeastOfGrads = 128;      // elements of the reduction to a cut
 constexpr int64_t kWantWaves = 2048;
 constexpr int64_t kFewRows = 1024;            // a block of classifier_join_kernel has four of them
 constexpr int64_t kThinPart = 4096;            // classes of a part of a row, at least, where rows are few
@@ -795,16 +794,19 @@ int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
 
 // How a product of M x N outputs over K is laid out: tiles of 256x256 where they fill most of the chip, the reduction cut
 // (into 1,024 elements at least) if need be, and little of them hangs over the edges; else of 128x128, the reduction cut
-// towards two blocks per CU, 256 elements to a cut at least.
+// towards one block per CU, `least` elements to a cut at least (0: not cut).  Two blocks per CU write twice the parts, which have to be added up: 64 x
+// 4,096 x 5,000 float32 83 + 156 us (loss + gradient) with two, 77 + 141 with one, 91 + 173 with a half; 333 x 515 x 10,007 float32 44 + 115, 44 + 108, 44 + 123.
+// z's parts are read by two kernels, so that its shortest cut is longer: 100 x 4,096 x 1,000 bf16 16 us with 256, 19 with 128,
+// the gradients 45.8 and 43.4.
 struct Layout { bool big; int64_t cuts, per_cut; };        // per_cut: elements of the reduction
-Layout lay_out(int64_t M, int64_t N, int64_t K, bool may_cut) {
+Layout lay_out(int64_t M, int64_t N, int64_t K, int64_t least) {
     Layout l = {};
     const int64_t big = ceil_div(M, kBigTile) * ceil_div(N, kBigTile), tiles = ceil_div(M, kTile) * ceil_div(N, kTile);
-    const int64_t big_cuts = may_cut && big < kChip ? std::max<int64_t>(1, std::min<int64_t>(kChip / big, K / 1024)) : 1;
+    const int64_t big_cuts = least > 0 && big < kChip ? std::max<int64_t>(1, std::min<int64_t>(kChip / big, K / 1024)) : 1;
     l.big = big * big_cuts * 4 >= kChip * 3 && M * N * 4 >= big * kBigTile * kBigTile * 3;
     int64_t want = 1;
     if (l.big) want = big_cuts;
-    else if (may_cut && tiles < kWantBlocks / 2) want = std::min<int64_t>(std::max<int64_t>(1, K / 256), kWantBlocks / tiles);
+    else if (least > 0 && tiles < kChip) want = std::min<int64_t>(std::max<int64_t>(1, K / least), kChip / tiles);
     l.per_cut = round_up(ceil_div(K, want), 64);
     l.cuts = ceil_div(K, l.per_cut);
     return l;
@@ -860,7 +862,7 @@ Plan plan_of(int dtype, int64_t rows, int64_t dim, int64_t classes, bool aligned
             p.thin_steps = (int)ceil_div(steps, p.thin_cuts * 4);
             p.thin_cuts = (int)ceil_div(steps, p.thin_steps * 4);
         } else {
-            p.thin_z = lay_out(rows, classes, dim, true);
+            p.thin_z = lay_out(rows, classes, dim, kLeastOfZ);
             p.thin_cuts = (int)p.thin_z.cuts;
         }
         p.z_ld = round_up(classes, 32);
@@ -870,7 +872,7 @@ Plan plan_of(int dtype, int64_t rows, int64_t dim, int64_t classes, bool aligned
         p.z_at = take(p.thin_cuts * rows * p.z_ld * 4);
     }
     if (!backward) {
-        p.z = lay_out(classes, rows, 1, false);
+        p.z = lay_out(classes, rows, 1, 0);
         p.z_tiles = ceil_div(classes, p.z.big ? kBigTile : kTile);
         p.sums_at = take(p.thin ? (p.thin_parts > 1 ? p.thin_parts * rows * 16 : 0) : p.z_tiles * rows * 16);
         p.target_at = take(rows * 4);
@@ -882,10 +884,10 @@ Plan plan_of(int dtype, int64_t rows, int64_t dim, int64_t classes, bool aligned
         const int64_t n = std::min(p.chunk, classes);
         p.dz_ld = planes_bytes(n);
         p.dz_at = take(rows * p.dz_ld);
-        p.z = lay_out(n, rows, 1, false);
+        p.z = lay_out(n, rows, 1, 0);
         p.z_tiles = p.thin ? ceil_div(rows, kThinBiasRows) : ceil_div(rows, p.z.big ? kBigTile : kTile);
-        p.dx = lay_out(rows, dim, n, true);
-        p.dw = lay_out(n, dim, rows, true);
+        p.dx = lay_out(rows, dim, n, kLeastOfGrads);
+        p.dw = lay_out(n, dim, rows, kLeastOfGrads);
         p.dx_at = take(p.chunks > 1 || p.dx.cuts > 1 ? p.dx.cuts * rows * dim * 4 : 0);
         p.dw_at = take(p.dw.cuts > 1 ? p.dw.cuts * n * dim * 4 : 0);
         p.db_at = take(p.z_tiles > 1 ? p.z_tiles * n * 4 : 0);
@@ -1056,10 +1058,10 @@ template <typename T> void backward(const ClassifierCall& c, const ClassifierGra
             ProfScope ps("classifier_dx", 2.0 * c.rows * n * c.dim, 6.0 * c.rows * n + (double)p.esz * (n + c.rows) * c.dim, st);
             if (parts_of_dx) {         // (later pieces of the classes are added to the first one's cuts, of which the last may have fewer)
                 g.out = (float*)(work + p.dx_at);
-                g.add = q > 0;
                 g.out_ld = c.dim;
                 g.out_cut = c.rows * c.dim;
-                launch_gemm<PRODUCT, P == 1 ? 2 : 3, P, true, false, float>(g, p.dx.per_cut, p.dx.big, st);
+                if (q == 0) launch_gemm<PRODUCT, P == 1 ? 2 : 3, P, true, false, float>(g, p.dx.per_cut, p.dx.big, st);
+                else launch_gemm<ADDED, P == 1 ? 2 : 3, P, true, false, float>(g, p.dx.per_cut, p.dx.big, st);
             } else {
                 g.out = d.dx;
                 g.out_ld = d.lddx;
