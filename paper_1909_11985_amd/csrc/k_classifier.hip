@@ -198,16 +198,18 @@ __device__ __forceinline__ void tile_of(const GemmArgs& g, int& tm, int& tn, int
     tm = (int)(first + l - (unsigned)tn * high);
 }
 
-// A block's waves, WM x WN, and a wave's 32x32 tiles, TM x TN.  64x64 to a wave read 4 KB of LDS for every 4 matrix
-// instructions, 128x64 read 6 KB for 8; what the larger tile needs is enough of them for the chip.
-struct Shape128 { static constexpr int WM = 2, WN = 2, TM = 2, TN = 2, SIDE = 128; };
+// A block's eight waves, WM x WN, and a wave's 32x32 tiles, TM x TN.  64x32 to a wave read 3 KB of LDS for every 2 matrix
+// instructions, 128x64 read 6 KB for 8; what the larger tile needs is enough of them for the chip.  (Four waves of 64x64 read 4 KB
+// for 4, but where a CU has one block its matrix cores wait with their only wave: gradients of 333 x 515 x 10,007 float32 115 us, with
+// eight 112; 100 x 4,096 x 1,000 bf16 44 and 42; 1,000 x 512 x 6,000 float32 155 and 147; with several blocks to a CU within 2 % either way.)
+struct Shape128 { static constexpr int WM = 2, WN = 4, TM = 2, TN = 1, SIDE = 128; };
 struct Shape256 { static constexpr int WM = 2, WN = 4, TM = 4, TN = 2, SIDE = 256; };
 // Elements of a reduction step and steps in LDS at a time, for PA and PB planes: long steps, because a step's part of a line
 // is asked for at once and parts of 32 bytes take the caches twice as long as parts of 64 (dw of 4,096 x 1,024 x 32,768 bf16:
 // 880 us with planes in groups of 16 elements, 594 with whole lines), and as many as fit, so that loads of the steps
 // to come are always in flight.
 template <int PA, int PB, int SIDE> struct Steps {
-    static constexpr int KS = PA + PB == 4 || (PA + PB == 6 && SIDE == 256) ? 16 : 32;
+    static constexpr int KS = (PA + PB == 4 || PA + PB == 6) && SIDE == 256 ? 16 : 32;
     static constexpr int STAGES = PA + PB == 2 || PA + PB == 4 ? 4 : 3;
 };
 
@@ -935,7 +937,7 @@ template <Want WANT, int PA, int PB, bool A_ALONG, bool B_ALONG, typename OUT> v
     g.group = big ? 4 : 8;
     const dim3 grid((unsigned)(g.tiles_m * g.tiles_n * ceil_div(g.steps, g.steps_per_cut)));
     if (big) hipLaunchKernelGGL((gemm_kernel<WANT, PA, PB, A_ALONG, B_ALONG, OUT, Shape256>), grid, dim3(512), 0, st, g);
-    else hipLaunchKernelGGL((gemm_kernel<WANT, PA, PB, A_ALONG, B_ALONG, OUT, Shape128>), grid, dim3(256), 0, st, g);
+    else hipLaunchKernelGGL((gemm_kernel<WANT, PA, PB, A_ALONG, B_ALONG, OUT, Shape128>), grid, dim3(512), 0, st, g);
 }
 constexpr int64_t kWhole = 1ll << 30;          // no cuts
 
