@@ -725,29 +725,42 @@ __global__ __launch_bounds__(256) void sum_slots_kernel(const float* __restrict_
     out[r * ld + (i - r * cols)] = Elem<OUT>::from_f32(s);
 }
 
+// Copies of x and w (either may be left out: no blocks) in one launch: a block has 256 work items of one of them.
+struct CopyOf { const void* src; char* dst; int64_t ld, n; unsigned blocks; };       // n: work items
+struct Copies { CopyOf x, w; };
+__device__ __forceinline__ bool copy_item(const Copies& a, CopyOf& c, int64_t& i) {
+    const bool first = blockIdx.x < a.x.blocks;
+    c = first ? a.x : a.w;
+    i = (int64_t)(blockIdx.x - (first ? 0 : a.x.blocks)) * 256 + threadIdx.x;
+    return i < c.n;
+}
+
 // rows of `cols` bf16 elements, copied to rows of `wide` (whole 16 bytes), zeros past them; a lane has 16 bytes
-__global__ __launch_bounds__(256) void pad_rows_kernel(const bf16_t* __restrict__ src, int64_t ld, int64_t cols, bf16_t* __restrict__ dst, int64_t wide, int64_t n) {
+__global__ __launch_bounds__(256) void pad_rows_kernel(Copies a, int64_t cols, int64_t wide) {
     constexpr int VEC = Elem<bf16_t>::VEC;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= n) return;
+    CopyOf o;
+    int64_t i;
+    if (!copy_item(a, o, i)) return;
     const int64_t vecs = wide / VEC, row = i / vecs, c = (i - row * vecs) * VEC;
+    const bf16_t* const src = (const bf16_t*)o.src + row * o.ld;
     Vec16<bf16_t> v;
     if (c + VEC <= cols) {
-        v = load_loose(src + row * ld + c);
+        v = load_loose(src + c);
     } else {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) v.e[e] = c + e < cols ? src[row * ld + c + e] : (bf16_t)0;
+        for (int e = 0; e < VEC; ++e) v.e[e] = c + e < cols ? src[c + e] : (bf16_t)0;
     }
-    store_vec(dst + row * wide + c, v);
+    store_vec((bf16_t*)o.dst + row * wide + c, v);
 }
 
 // rows of float32 as three planes, zeros up to whole groups; a lane has four elements.  (What rounds to more than bf16
 // holds takes its largest number first.)
-__global__ __launch_bounds__(256) void split_rows_kernel(const float* __restrict__ src, int64_t ld, int64_t cols, char* __restrict__ dst, int64_t dst_ld, int64_t n) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= n) return;
+__global__ __launch_bounds__(256) void split_rows_kernel(Copies a, int64_t cols, int64_t dst_ld) {
+    CopyOf o;
+    int64_t i;
+    if (!copy_item(a, o, i)) return;
     const int64_t quads = dst_ld / kGroupBytes * (kGroup / 4), row = i / quads, c = (i - row * quads) * 4;
-    const float* const p = src + row * ld + c;
+    const float* const p = (const float*)o.src + row * o.ld + c;
     float v[4];
     if (c + 4 <= cols) {
         const Vec16<float> t = load_loose(p);
@@ -758,7 +771,7 @@ __global__ __launch_bounds__(256) void split_rows_kernel(const float* __restrict
         for (int e = 0; e < 4; ++e) v[e] = c + e < cols ? p[e] : 0.f;
     }
     const float most = __uint_as_float(0x7f7f0000u);
-    char* const to = dst + row * dst_ld + plane_at(c);
+    char* const to = o.dst + row * dst_ld + plane_at(c);
     float high[4], rest[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -833,7 +846,7 @@ struct Plan {
     Layout z, dx, dw;
     int64_t z_tiles;           // of classes (forward), of rows (backward)
     // workspace
-    int64_t x_at, w_at, xs_at, ws_at, z_at, sums_at, target_at, dz_at, dz_ld, dx_at, dw_at, db_at, bytes;
+    int64_t x_at, w_at, z_at, sums_at, target_at, dz_at, dz_ld, dx_at, dw_at, db_at, bytes;
 };
 
 Plan plan_of(int dtype, int64_t rows, int64_t dim, int64_t classes, bool aligned_x, bool aligned_w, bool backward) {
@@ -852,10 +865,8 @@ Plan plan_of(int dtype, int64_t rows, int64_t dim, int64_t classes, bool aligned
     p.pad_w = p.tiles && dtype == 1 && !aligned_w;
     p.split = p.tiles && dtype != 1;
     p.split_ld = planes_bytes(dim);
-    p.x_at = take(p.pad_x ? rows * p.wide * p.esz : 0);
-    p.w_at = take(p.pad_w ? classes * p.wide * p.esz : 0);
-    p.xs_at = take(p.split ? rows * p.split_ld : 0);
-    p.ws_at = take(p.split ? classes * p.split_ld : 0);
+    p.x_at = take(p.split ? rows * p.split_ld : p.pad_x ? rows * p.wide * p.esz : 0);
+    p.w_at = take(p.split ? classes * p.split_ld : p.pad_w ? classes * p.wide * p.esz : 0);
     if (p.thin) {
         if (p.narrow) {
             const int64_t steps = ceil_div(dim * p.esz, kStepBytes);
@@ -905,23 +916,27 @@ bool lies_aligned(const void* p, int64_t ld, int64_t dim, int esz) {
 // x and w as operands whose reduction lies along them
 struct Inputs { Operand x, w; };
 template <typename T> Inputs inputs_of(const ClassifierCall& c, const Plan& p, char* work, hipStream_t st) {
-    auto operand = [&](const void* src, int64_t ld, int64_t rows, bool pad, int64_t pad_at, int64_t split_at) {
-        if (!p.tiles) return Operand{};
-        if (sizeof(T) == 4) {
-            const int64_t n = rows * (p.split_ld / kGroupBytes * (kGroup / 4));
-            ProfScope ps("classifier_split", 0.0, (4.0 * c.dim + p.split_ld) * rows, st);
-            hipLaunchKernelGGL(split_rows_kernel, dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, st, (const float*)src, ld, c.dim, work + split_at, p.split_ld, n);
-            return Operand{work + split_at, p.split_ld, rows, round_up(c.dim, 16), 3};
-        }
-        if (!pad) return Operand{(const char*)src, ld * 2, rows, p.wide, 1};
-        const int64_t n = rows * (p.wide / 8);
-        ProfScope ps("classifier_pad", 0.0, 2.0 * rows * (c.dim + p.wide), st);
-        hipLaunchKernelGGL(pad_rows_kernel, dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, st, (const bf16_t*)src, ld, c.dim, (bf16_t*)(work + pad_at), p.wide, n);
-        return Operand{work + pad_at, p.wide * 2, rows, p.wide, 1};
+    if (!p.tiles) return Inputs{};
+    const int64_t items = p.split ? p.split_ld / kGroupBytes * (kGroup / 4) : p.wide / 8;        // of a row
+    Copies a = {};
+    int64_t rows = 0;
+    auto operand = [&](const void* src, int64_t ld, int64_t n, bool pad, int64_t copy_at, CopyOf& copy) {
+        if (!p.split && !pad) return Operand{(const char*)src, ld * 2, n, p.wide, 1};
+        rows += n;
+        copy = CopyOf{src, work + copy_at, ld, n * items, (unsigned)ceil_div(n * items, 256)};
+        return p.split ? Operand{copy.dst, p.split_ld, n, round_up(c.dim, 16), 3} : Operand{copy.dst, p.wide * 2, n, p.wide, 1};
     };
     Inputs in;
-    in.x = operand(c.x, c.ldx, c.rows, p.pad_x, p.x_at, p.xs_at);
-    in.w = operand(c.w, c.ldw, c.classes, p.pad_w, p.w_at, p.ws_at);
+    in.x = operand(c.x, c.ldx, c.rows, p.pad_x, p.x_at, a.x);
+    in.w = operand(c.w, c.ldw, c.classes, p.pad_w, p.w_at, a.w);
+    const dim3 grid(a.x.blocks + a.w.blocks);
+    if (p.split) {
+        ProfScope ps("classifier_split", 0.0, (4.0 * c.dim + p.split_ld) * rows, st);
+        hipLaunchKernelGGL(split_rows_kernel, grid, dim3(256), 0, st, a, c.dim, p.split_ld);
+    } else if (rows > 0) {
+        ProfScope ps("classifier_pad", 0.0, 2.0 * rows * (c.dim + p.wide), st);
+        hipLaunchKernelGGL(pad_rows_kernel, grid, dim3(256), 0, st, a, c.dim, p.wide);
+    }
     return in;
 }
 // the same memory with its lines the reduction: `rows` outputs (up to whole pieces) by `k` lines
