@@ -800,7 +800,10 @@ constexpr int64_t kMostAtOnce = 1 << 20;       // classes of it: offsets in a ti
 constexpr int64_t kWantBlocks = 512;           // of thin_sums_kernel
 constexpr int64_t kChip = 256;                 // CUs: a block of a product each
 constexpr int64_t kLeastOfZ = 256, kLeastOfGrads = 128;      // elements of the reduction to a cut
-constexpr int64_t kWantWaves = 2048;
+constexpr int64_t kWantWaves = 2048;           // of thin_logits_kernel, or more:
+// a wave's steps at most.  Of longer ones the last few of many blocks take long alone; shorter ones write more parts: 1 x 4,096 x
+// 100,000 float32 353 us without a limit, 314, 313, 324 and 397 with 16, 12, 8 and 4; 3 x 3,782 x 41,732 165, 152, 153, 153 and 162.
+constexpr int64_t kMostSteps = 12;
 constexpr int64_t kFewRows = 1024;            // a block of classifier_join_kernel has four of them
 constexpr int64_t kThinPart = 4096;            // classes of a part of a row, at least, where rows are few
 
@@ -870,7 +873,7 @@ Plan plan_of(int dtype, int64_t rows, int64_t dim, int64_t classes, bool aligned
     if (p.thin) {
         if (p.narrow) {
             const int64_t steps = ceil_div(dim * p.esz, kStepBytes);
-            const int64_t waves = std::max<int64_t>(4, std::min<int64_t>(kWantWaves / ceil_div(classes, 32), steps));
+            const int64_t waves = std::max<int64_t>(4, std::min<int64_t>(std::max(kWantWaves / ceil_div(classes, 32), ceil_div(steps, kMostSteps)), steps));
             p.thin_cuts = (int)std::max<int64_t>(1, waves / 4);
             p.thin_steps = (int)ceil_div(steps, p.thin_cuts * 4);
             p.thin_cuts = (int)ceil_div(steps, p.thin_steps * 4);
