@@ -469,11 +469,12 @@ int32_t edl_log_probs(int32_t dtype, const void* dev_logits, int64_t ld, int64_t
                       void* dev_work, size_t work_bytes, void* hip_stream);
 
 /* Gradient of the logits for gradients g = dev_dlog_prob[rows] of log_prob and h = dev_dentropy[rows] of entropy (either may be
- * NULL: zeros), from what edl_log_probs left:
+ * NULL: zeros), from what edl_log_probs left for these logits:
  *   dlogits = g (1[class = target] - p) - h p (log p + entropy)
  * in dtype, rounded once; dev_dlogits may be dev_logits (with the same ld).  Masked classes get 0, unless one is the target (g).
- * Rows without a target take g = 0; a row with g = h = 0 gets zeros whatever its logits are.  dev_targets may be NULL if
- * dev_dlog_prob is, dev_entropy if dev_dentropy is.  Errors as above. */
+ * Rows without a target take g = 0; a row with g = h = 0 gets zeros whatever its logits are.  log p is a logit less the row's lse;
+ * where lse is 128 or more away from 0, and float32 no longer holds the sum's logarithm in it, the row's sums are formed again from its
+ * logits, which are then read twice.  dev_targets may be NULL if dev_dlog_prob is, dev_entropy if dev_dentropy is.  Errors as above. */
 int32_t edl_log_probs_backward(int32_t dtype, const void* dev_logits, int64_t ld, int64_t rows, int64_t classes, const int32_t* dev_targets,
                                const float* dev_lse, const float* dev_entropy, const float* dev_dlog_prob, const float* dev_dentropy,
                                void* dev_dlogits, int64_t ldd, void* hip_stream);

@@ -402,7 +402,7 @@ __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmAr
 #pragma unroll
                 for (int i = 0; i < TM; ++i)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) acc[i][j][e] = row.of(acc[i][j][e], place(i, e) == hot);
+                    for (int e = 0; e < 16; ++e) acc[i][j][e] = row.of<false>(acc[i][j][e], place(i, e) == hot);
             }
             const int c = threadIdx.x % PIECES, rows = (int)min((int64_t)SIDE, g.b.rows - n0);
             const bool wanted = m0 + c * 8 < g.dz_classes;
@@ -634,7 +634,7 @@ __global__ __launch_bounds__(256) void thin_grads_kernel(ThinRows g, char* dz, i
         const LogitGrad grad = logit_grad(g.facts, row, g.classes);
         const float z[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) d[e] = c + e < g.classes ? grad.of(z[e], c + e == grad.target) : 0.f;
+        for (int e = 0; e < 4; ++e) d[e] = c + e < g.classes ? grad.of<false>(z[e], c + e == grad.target) : 0.f;
     }
     store_planes(dz + row * dz_ld, c, d);
 }

@@ -45,7 +45,7 @@ struct DropoutArgs {
 template <typename T, int U>
 __global__ __launch_bounds__(256) void dropout_kernel(const T* x, T* y, DropoutArgs a) {
     int64_t at0;
-    const int64_t row0 = block_first_row<U>(a.m, at0);
+    const int64_t row0 = block_first_row<U>(a.m, at0, blockIdx.x);
     // addresses and draws from the block's first row on, which are the same for all lanes, in 32x32-bit products
     const T* const x0 = x + row0 * a.ldx;
     T* const y0 = y + row0 * a.ldy;

@@ -11,7 +11,7 @@
 // for each of a lane's 32 logits: 11 KB of instructions, whose first fetch alone took most of the 13 us of a call for one row.
 //
 // Measured: 4,096 x 49,999 bf16 with 10 alternatives 114 us (3.6 TB/s), 8,192 x 32,768 bf16 without 122 us (4.4 TB/s) and their
-// gradient 210 us (5.1 TB/s); 1 x 32,000 bf16 with 5 in eight parts 8 + 4 us; 256 x 1,000 float32 with 5, a wave to a row, 6 us.
+// gradient 216 us (5.0 TB/s) and 5 for the launch that looks for rows whose lse is far (444 in all if every row is); 1 x 32,000 bf16 with 5 in eight parts 8 + 4 us; 256 x 1,000 float32 with 5, a wave to a row, 6 us.
 #include <algorithm>
 
 #include "operators.h"
@@ -210,13 +210,106 @@ struct GradArgs {
     Pieces m;
     int64_t ld, ldd;
     RowFacts facts;
+    unsigned far_blocks;       // for the rows whose lse is far
+    bool far_by_wave;          // a wave has such a row, else a block
 };
 
-// Element-wise once the row's numbers are known, which its lanes read from cache.
+// Rows whose lse is far (softmax_sums.h): their sums, then their gradient, by a wave or a block of 256 for each such row, since
+// dlogits may lie where the logits do.  Rows are dealt out one by one, so that a run of far ones spreads over the chip; a
+// lane looks at one row at a time.
+template <typename T, int LANES>
+__device__ __forceinline__ void far_rows_by(const T* logits, T* dlogits, const GradArgs& a, unsigned block) {
+    constexpr int U = 2, WIDE = LANES * kPiece;
+    __shared__ float4 wave_sums[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int me = LANES == 64 ? lane : (int)threadIdx.x;
+    const int64_t groups = (int64_t)a.far_blocks * (256 / LANES), group = (int64_t)block * (256 / LANES) + (LANES == 64 ? wave : 0);
+    for (int64_t first = group; first < a.m.rows; first += groups * 64) {
+        // (each wave of a block looks at the same 64 rows)
+        const int64_t look = first + lane * groups;
+        for (uint64_t left = __ballot(look < a.m.rows && logit_grad(a.facts, min(look, a.m.rows - 1), a.m.cols).far); left != 0; left &= left - 1) {
+            const int64_t row = first + (int64_t)__builtin_ctzll(left) * groups;
+            const T* const z = logits + row * a.ld;
+            T* const d = dlogits + row * a.ldd;
+            SoftmaxSums sums;
+            for (int64_t at = me * kPiece; at < a.m.cols; at += U * WIDE) {
+                float v[U][kPiece], m = sums.m;
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int64_t c = at + u * WIDE;
+                    if (c + kPiece <= a.m.cols) {
+                        load_piece(z + c, v[u]);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < kPiece; ++e) v[u][e] = c + e < a.m.cols ? Elem<T>::to_f32(z[c + e]) : -INFINITY;
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int e = 0; e < kPiece; ++e) m = fmaxf(m, v[u][e]);
+                softmax_rebase(sums, m);
+                const float base = softmax_base(sums);
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int e = 0; e < kPiece; ++e) softmax_add(sums, v[u][e], base);
+            }
+            softmax_join_wave(sums);
+            if (LANES == 256) {
+                if (lane == 0) wave_sums[wave] = make_float4(sums.m, sums.s, sums.t, 0.f);
+                __syncthreads();
+                SoftmaxSums all;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    SoftmaxSums o;
+                    o.m = wave_sums[w].x; o.s = wave_sums[w].y; o.t = wave_sums[w].z;
+                    softmax_join(all, o);
+                }
+                sums = all;
+                __syncthreads();       // (the next row writes them again)
+            }
+            LogitGrad grad = logit_grad(a.facts, row, a.m.cols);
+            const float2 far = far_base(sums);
+            grad.base = far.x;
+            grad.low = far.y;
+            for (int64_t c = me * kPiece; c < a.m.cols; c += WIDE) {
+                const int64_t hot = grad.target - c;
+                if (c + kPiece <= a.m.cols) {
+                    float v[kPiece];
+                    load_piece(z + c, v);
+#pragma unroll
+                    for (int e = 0; e < kPiece; ++e) v[e] = grad.template of<true>(v[e], e == hot);
+                    store_piece(d + c, v);
+                } else {
+                    for (int e = 0; c + e < a.m.cols; ++e) d[c + e] = Elem<T>::from_f32(grad.template of<true>(Elem<T>::to_f32(z[c + e]), e == hot));
+                }
+            }
+        }
+    }
+}
+
+template <typename T> __device__ __forceinline__ void far_rows(const T* logits, T* dlogits, const GradArgs& a, unsigned block) {
+    if (a.far_by_wave) far_rows_by<T, 64>(logits, dlogits, a, block);
+    else far_rows_by<T, 256>(logits, dlogits, a, block);
+}
+template <typename T> __global__ __launch_bounds__(256) void far_rows_kernel(const T* logits, T* dlogits, GradArgs a) { far_rows(logits, dlogits, a, blockIdx.x); }
+
+// Element-wise once the row's numbers are known, which its lanes read from cache.  Of small calls (U = 1) the first blocks have the rows
+// whose lse is far, which spares them a launch; large ones leave those to far_rows_kernel, because with its code beside this
+// one 8,192 x 32,768 bf16 takes 250 us, without 216.
 template <typename T, int U>
 __global__ __launch_bounds__(256) void log_probs_grad_kernel(const T* logits, T* dlogits, GradArgs a) {
+    unsigned block = blockIdx.x;
+    if constexpr (U == 1) {
+        if (block < a.far_blocks) {
+            far_rows(logits, dlogits, a, block);
+            return;
+        }
+        block -= a.far_blocks;
+    }
     int64_t at0;
-    const int64_t row0 = block_first_row<U>(a.m, at0);
+    const int64_t row0 = block_first_row<U>(a.m, at0, block);
     const T* const z0 = logits + row0 * a.ld;
     T* const d0 = dlogits + row0 * a.ldd;
     const int64_t rows_left = a.m.rows - row0;
@@ -231,8 +324,9 @@ __global__ __launch_bounds__(256) void log_probs_grad_kernel(const T* logits, T*
     for (int u = 0; u < U; ++u) {
         if (q[u].row >= rows_left) return;
         const LogitGrad row = logit_grad(a.facts, row0 + q[u].row, a.m.cols);
+        if (row.far) continue;         // far_rows has it
         const int64_t hot = row.target - q[u].col;
-        auto grad = [&](float z, int e) { return row.of(z, e == hot); };
+        auto grad = [&](float z, int e) { return row.template of<false>(z, e == hot); };
         T* pd = d0 + (uint64_t)q[u].row * (uint32_t)a.ldd + q[u].col;
         if (q[u].col + kPiece <= a.m.cols) {
 #pragma unroll
@@ -251,6 +345,7 @@ __global__ __launch_bounds__(256) void log_probs_grad_kernel(const T* logits, T*
 constexpr int64_t kSmallGradItems = 1 << 18;     // (as in k_dropout.hip)
 constexpr int64_t kWaveClasses = 1024;           // rows up to this length are a wave's
 constexpr int64_t kPartClasses = 4096, kMaxParts = 64, kWantBlocks = 1024;
+constexpr int64_t kMostFarBlocks = 1024;         // four to a CU
 
 }  // namespace
 
@@ -318,14 +413,22 @@ void launch_log_probs_grad(int dtype, const void* logits, int64_t ld, int64_t ro
     a.ldd = ldd;
     a.facts = RowFacts{targets, lse, entropy, dlog_prob, dentropy};
     const double esz = dtype == 1 ? 2.0 : 4.0;
-    ProfScope ps("log_probs_grad", 0.0, 2.0 * esz * (double)rows * (double)classes, st);
     const int64_t items = rows * a.m.per_row;
     const bool small = items < kSmallGradItems;
-    const unsigned grid = (unsigned)((items + (small ? 255 : 1023)) / (small ? 256 : 1024));
+    a.far_by_wave = classes <= kWaveClasses;
+    a.far_blocks = (unsigned)std::min(kMostFarBlocks, a.far_by_wave ? (rows + 3) / 4 : rows);
+    const unsigned grid = (unsigned)((items + (small ? 255 : 1023)) / (small ? 256 : 1024)) + (small ? a.far_blocks : 0);
+    {
+        ProfScope ps("log_probs_grad", 0.0, 2.0 * esz * (double)rows * (double)classes, st);
 #define EDL_LOG_PROBS_GRAD(TT, UU) hipLaunchKernelGGL((log_probs_grad_kernel<TT, UU>), dim3(grid), dim3(256), 0, st, (const TT*)logits, (TT*)dlogits, a)
-    if (dtype == 1) { if (small) EDL_LOG_PROBS_GRAD(bf16_t, 1); else EDL_LOG_PROBS_GRAD(bf16_t, 4); }
-    else { if (small) EDL_LOG_PROBS_GRAD(float, 1); else EDL_LOG_PROBS_GRAD(float, 4); }
+        if (dtype == 1) { if (small) EDL_LOG_PROBS_GRAD(bf16_t, 1); else EDL_LOG_PROBS_GRAD(bf16_t, 4); }
+        else { if (small) EDL_LOG_PROBS_GRAD(float, 1); else EDL_LOG_PROBS_GRAD(float, 4); }
 #undef EDL_LOG_PROBS_GRAD
+    }
+    if (small) return;
+    ProfScope ps("log_probs_far_rows", 0.0, 0.0, st);
+    if (dtype == 1) hipLaunchKernelGGL((far_rows_kernel<bf16_t>), dim3(a.far_blocks), dim3(256), 0, st, (const bf16_t*)logits, (bf16_t*)dlogits, a);
+    else hipLaunchKernelGGL((far_rows_kernel<float>), dim3(a.far_blocks), dim3(256), 0, st, (const float*)logits, (float*)dlogits, a);
 }
 
 }  // namespace edl

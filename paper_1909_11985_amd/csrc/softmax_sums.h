@@ -60,18 +60,25 @@ __device__ __forceinline__ float softmax_entropy(const SoftmaxSums& a) { return 
 __device__ __forceinline__ float softmax_log_prob(const SoftmaxSums& a, float z) { return a.s == 0.f ? -INFINITY : (z - a.m) - log2f(a.s) * kLn2; }
 
 // ---- the gradient of a logit ---------------------------------------------------------------------------------------------
-// What a row's logits need: dz = g (1[c = t] - p) - h p (log p + H).
+// What a row's logits need: dz = g (1[c = t] - p) - h p (log p + H), with log p = (z - base) - low.
+// Forward leaves lse, one float32: base, with low = 0.  p is then off by up to half a step of lse (2^-24 of it at most), and
+// where log s is below lse's last place, p is off by the factor s: rows of the lowest value alone have lse = m, and so p = 1.
+// Rows whose lse is at least kFarLse away from 0 take base = m and low = log s instead, summed up again from their logits; below it
+// the half step is 2^-18 at most.
+constexpr float kFarLse = 128.f;
 struct RowFacts {              // of each row; null: none (targets), zeros (gradients)
     const int32_t* targets;
     const float *lse, *entropy, *dlog_prob, *dentropy;
 };
 struct LogitGrad {
-    float g, h, lse, both;
+    float g, h, base, low, both;
     int64_t target;            // -1: none
     bool none;                 // zeros, whatever the logits are
+    bool far;                  // base and low are yet to be had from the logits
 
-    __device__ __forceinline__ float of(float z, bool hot) const {
-        const float lp = z - lse, p = exp2_of(lp * kLog2e);
+    // FAR: rows may be far, or low is known to be 0 (an operation less for each logit)
+    template <bool FAR> __device__ __forceinline__ float of(float z, bool hot) const {
+        const float lp = FAR ? (z - base) - low : z - base, p = exp2_of(lp * kLog2e);
         const float d = z == -INFINITY ? 0.f : p * (both - h * fmaxf(lp, kFarBelow));
         return none ? 0.f : hot ? d + g : d;
     }
@@ -83,11 +90,15 @@ __device__ __forceinline__ LogitGrad logit_grad(const RowFacts& f, int64_t row, 
     r.target = has ? t : -1;
     r.g = has && f.dlog_prob != nullptr ? f.dlog_prob[row] : 0.f;
     r.h = f.dentropy != nullptr ? f.dentropy[row] : 0.f;
-    r.lse = f.lse[row];
+    r.base = f.lse[row];
+    r.low = 0.f;
     r.both = -(r.g + (r.h != 0.f ? r.h * f.entropy[row] : 0.f));
     r.none = r.g == 0.f && r.h == 0.f;
+    r.far = !r.none && fabsf(r.base) >= kFarLse && fabsf(r.base) < INFINITY;       // (infinite or not a number: as good as it gets)
     return r;
 }
+// what a row that is far takes, from the sums over all of its logits
+__device__ __forceinline__ float2 far_base(const SoftmaxSums& a) { return make_float2(a.m, log2f(a.s) * kLn2); }
 
 // ---- the k largest of a row, one per lane of a wave, best first -------------------------------------------------------
 // Ordered by value, then by the lower class: both in one 64-bit key, so that the result does not depend on the order in

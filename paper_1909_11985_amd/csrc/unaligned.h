@@ -31,8 +31,8 @@ struct Piece {
     int64_t col;
 };
 // The block's first row; `at0` receives its first piece in that row.  One division for the block.
-template <int U> __device__ __forceinline__ int64_t block_first_row(const Pieces& p, int64_t& at0) {
-    const int64_t item0 = (int64_t)blockIdx.x * (256 * U);
+template <int U> __device__ __forceinline__ int64_t block_first_row(const Pieces& p, int64_t& at0, unsigned block) {
+    const int64_t item0 = (int64_t)block * (256 * U);
     const int64_t row0 = item0 / p.per_row;
     at0 = item0 - row0 * p.per_row;
     return row0;
