@@ -495,7 +495,7 @@ int32_t edl_classifier_log_probs(int32_t dtype, const void* dev_x, int64_t ldx, 
                                  void* dev_work, size_t work_bytes, void* hip_stream);
 
 /* Gradients for gradients g = dev_dlog_prob[rows] of log_prob and h = dev_dentropy[rows] of entropy (either may be NULL: zeros):
- * with dz as in edl_log_probs_backward, dx = dz w in dtype, dw = dz^T x and dbias = sum of dz over the rows in float32 (what
+ * with dz as in edl_log_probs_backward (of rows whose lse is 128 or more away from 0, sums over the classes are formed again), dx = dz w in dtype, dw = dz^T x and dbias = sum of dz over the rows in float32 (what
  * edl_average_update and edl_adam_update take; dev_dbias may be NULL).  The logits are formed again, a piece of the classes at a
  * time, and dz is stored for such a piece (at most 1 GiB of workspace, or 128 classes) as a sum of three bf16 numbers, so that dw and
  * dbias are float32 results.  All outputs are written, not added to, and must not

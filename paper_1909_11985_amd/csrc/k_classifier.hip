@@ -14,7 +14,9 @@
 // products of planes that are not below float32's last place.  The matrix cores do 16 bf16 multiplications in the time of one float32 one,
 // so six of them still take less than half of its time.
 //
-// The gradient forms z again rather than keep it, a piece of the classes at a time.  dz is stored for the two products that
+// The gradient forms z again rather than keep it, a piece of the classes at a time.  Rows whose lse is far (softmax_sums.h) need
+// their largest logit and sum first: of z in float32 parts, the block that forms their dz sums them up; on tiles the loss's product and join
+// run once more, for the tiles that have such a row alone (5 + 2 us of launches that do nothing where there is none).  dz is stored for the two products that
 // read it, in both types as three planes: dw is float32, and a single rounding of dz to bf16 would be its largest error by
 // four orders of magnitude.  dx of bf16, which is rounded to bf16 itself, takes the first two.
 //
@@ -171,8 +173,9 @@ struct GemmArgs {
     const float* bias;
     int64_t first_class, classes, all_classes;     // classes: the end of this launch's
     RowFacts facts;
+    const float2* far;         // dz: of rows whose lse is far, LogitGrad's base and low
     float4* sums;              // [tile of classes][rows]: m, s, t
-    float* target_z;
+    float* target_z;           // null: not wanted
     char* dz;                  // [rows][dz_ld bytes] of the classes from first_class on, three planes
     int64_t dz_ld;
     int dz_classes;            // up to whole pairs of pieces (zeros past the last class)
@@ -213,18 +216,18 @@ template <int PA, int PB, int SIDE> struct Steps {
     static constexpr int STAGES = PA + PB == 2 || PA + PB == 4 ? 4 : 3;
 };
 
+template <int PA, int PB, int SIDE> constexpr int lds_bytes() { return Steps<PA, PB, SIDE>::STAGES * (PA + PB) * SIDE * Steps<PA, PB, SIDE>::KS * 2; }
+// One tile, by a block; smem: lds_bytes of LDS.
 template <Want WANT, int PA, int PB, bool A_ALONG, bool B_ALONG, typename OUT, typename SHAPE>
-__global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmArgs g) {
+__device__ __forceinline__ void gemm_tile(const GemmArgs& g, int tm, int tn, int cut, char* smem) {
     constexpr int WM = SHAPE::WM, WN = SHAPE::WN, TM = SHAPE::TM, TN = SHAPE::TN, THREADS = WM * WN * 64, SIDE = SHAPE::SIDE;
     constexpr int KS = Steps<PA, PB, SIDE>::KS, STAGES = Steps<PA, PB, SIDE>::STAGES;
     typedef Tile<A_ALONG, SIDE, PA, KS, THREADS> TA;
     typedef Tile<B_ALONG, SIDE, PB, KS, THREADS> TB;
     constexpr int STAGE = TA::BYTES + TB::BYTES;
-    __shared__ __attribute__((aligned(16))) char smem[STAGES * STAGE];
+    static_assert(STAGES * STAGE == lds_bytes<PA, PB, SIDE>(), "what the kernel holds");
     const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
-    int tm, tn, cut;
-    tile_of(g, tm, tn, cut);
     const int64_t m0 = (int64_t)tm * SIDE, n0 = (int64_t)tn * SIDE;
     const int first = cut * g.steps_per_cut, all = min(g.steps_per_cut, g.steps - first);
     TA ta;
@@ -351,7 +354,7 @@ __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmAr
             for (int j = 0; j < TN; ++j) {
                 const int col = (wn * TN + j) * 32 + (lane & 31);
                 const int64_t n = n0 + col;
-                const int64_t t = n < g.b.rows && g.facts.targets != nullptr ? g.facts.targets[n] : -1;
+                const int64_t t = n < g.b.rows && g.facts.targets != nullptr && g.target_z != nullptr ? g.facts.targets[n] : -1;
                 const int hot = place_of(t);
                 SoftmaxSums s;
 #pragma unroll
@@ -397,12 +400,24 @@ __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmAr
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
                 const int64_t n = n0 + (wn * TN + j) * 32 + (lane & 31);
-                const LogitGrad row = logit_grad(g.facts, min(n, g.b.rows - 1), g.all_classes);
+                LogitGrad row = logit_grad(g.facts, min(n, g.b.rows - 1), g.all_classes);
                 const int hot = place_of(row.target);
+                if (__ballot(row.far) == 0) {
+#pragma unroll
+                    for (int i = 0; i < TM; ++i)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) acc[i][j][e] = row.of<false>(acc[i][j][e], place(i, e) == hot);
+                    continue;
+                }
+                if (row.far) {
+                    const float2 far = g.far[min(n, g.b.rows - 1)];
+                    row.base = far.x;
+                    row.low = far.y;
+                }
 #pragma unroll
                 for (int i = 0; i < TM; ++i)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) acc[i][j][e] = row.of<false>(acc[i][j][e], place(i, e) == hot);
+                    for (int e = 0; e < 16; ++e) acc[i][j][e] = row.of<true>(acc[i][j][e], place(i, e) == hot);
             }
             const int c = threadIdx.x % PIECES, rows = (int)min((int64_t)SIDE, g.b.rows - n0);
             const bool wanted = m0 + c * 8 < g.dz_classes;
@@ -450,6 +465,33 @@ __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmAr
                     g.db[tn * g.db_ld + m0 + threadIdx.x] = sum;
                 }
             }
+        }
+    }
+}
+
+template <Want WANT, int PA, int PB, bool A_ALONG, bool B_ALONG, typename OUT, typename SHAPE>
+__global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void gemm_kernel(GemmArgs g) {
+    __shared__ __attribute__((aligned(16))) char smem[lds_bytes<PA, PB, SHAPE::SIDE>()];
+    int tm, tn, cut;
+    tile_of(g, tm, tn, cut);
+    gemm_tile<WANT, PA, PB, A_ALONG, B_ALONG, OUT, SHAPE>(g, tm, tn, cut, smem);
+}
+
+// z's sums, of tiles with a row whose lse is far.  Mostly there is none: a block looks at the rows of its tiles once, and has all
+// tiles of those rows, or every gridDim / tiles_n-th of them.  (With a block to each tile 2,048 of them take 25 us where none
+// is wanted, so 5.)
+template <int P, typename SHAPE> __global__ __launch_bounds__(SHAPE::WM * SHAPE::WN * 64) void far_sums_kernel(GemmArgs g) {
+    __shared__ __attribute__((aligned(16))) char smem[lds_bytes<P, P, SHAPE::SIDE>()];
+    const int wide = min(g.tiles_n, (int)gridDim.x), deep = (int)gridDim.x / wide;
+    if ((int)blockIdx.x >= wide * deep) return;
+    for (int tn = (int)blockIdx.x % wide; tn < g.tiles_n; tn += wide) {
+        bool any = false;
+        for (int64_t n = (int64_t)tn * SHAPE::SIDE + (threadIdx.x & 63); n < min((int64_t)(tn + 1) * SHAPE::SIDE, g.b.rows); n += 64)
+            any = any || row_is_far(g.facts, n, g.all_classes);
+        if (__ballot(any) == 0) continue;          // (every wave looks at all of them)
+        for (int tm = (int)blockIdx.x / wide; tm < g.tiles_m; tm += deep) {
+            gemm_tile<SUMS, P, P, true, true, float, SHAPE>(g, tm, tn, 0, smem);
+            __syncthreads();           // the next tile's loads take the place of this one's sums
         }
     }
 }
@@ -583,14 +625,9 @@ __device__ __forceinline__ void write_results(const RowResults& out, const int32
     const int32_t t = targets[row];
     out.log_prob[row] = t >= 0 && t < classes ? softmax_log_prob(s, zt) : 0.f;
 }
-// Sums of a part of a row's classes; of all of them, the results.
-__global__ __launch_bounds__(256) void thin_sums_kernel(ThinRows g, int parts, int64_t part, float4* sums, float* target_z, RowResults out) {
+// Sums of a row's classes [lo, hi), by a block: all of its threads have them.  at(class, logit) is called for each.
+template <typename F> __device__ __forceinline__ SoftmaxSums thin_row_sums(const ThinRows& g, int64_t row, int64_t lo, int64_t hi, F at) {
     __shared__ float4 wave_sums[4];
-    __shared__ float target;
-    const int64_t row = blockIdx.x / (unsigned)parts;
-    const int p = (int)(blockIdx.x - (unsigned)row * (unsigned)parts);
-    const int64_t lo = p * part, hi = min(lo + part, g.classes);
-    const int64_t t = g.facts.targets != nullptr ? g.facts.targets[row] : -1;
     SoftmaxSums s;
     for (int64_t c = lo + threadIdx.x * 4; c < hi; c += 1024) {
         const float4 v = thin_logits(g, row, c);
@@ -598,11 +635,8 @@ __global__ __launch_bounds__(256) void thin_sums_kernel(ThinRows g, int parts, i
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             if (c + e >= hi) z[e] = -INFINITY;
+            else at(c + e, z[e]);
             m = fmaxf(m, z[e]);
-            if (c + e == t && c + e < hi) {
-                if (parts == 1) target = z[e];
-                else target_z[row] = z[e];
-            }
         }
         softmax_rebase(s, m);
         const float base = softmax_base(s);
@@ -612,29 +646,51 @@ __global__ __launch_bounds__(256) void thin_sums_kernel(ThinRows g, int parts, i
     softmax_join_wave(s);
     if ((threadIdx.x & 63) == 0) wave_sums[threadIdx.x >> 6] = make_float4(s.m, s.s, s.t, 0.f);
     __syncthreads();
-    if (threadIdx.x != 0) return;
-    for (int w = 1; w < 4; ++w) {
+    SoftmaxSums all;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
         SoftmaxSums o;
         o.m = wave_sums[w].x; o.s = wave_sums[w].y; o.t = wave_sums[w].z;
-        softmax_join(s, o);
+        softmax_join(all, o);
     }
+    return all;
+}
+// Sums of a part of a row's classes; of all of them, the results.
+__global__ __launch_bounds__(256) void thin_sums_kernel(ThinRows g, int parts, int64_t part, float4* sums, float* target_z, RowResults out) {
+    __shared__ float target;
+    const int64_t row = blockIdx.x / (unsigned)parts;
+    const int p = (int)(blockIdx.x - (unsigned)row * (unsigned)parts);
+    const int64_t lo = p * part, hi = min(lo + part, g.classes);
+    const int64_t t = g.facts.targets != nullptr ? g.facts.targets[row] : -1;
+    const SoftmaxSums s = thin_row_sums(g, row, lo, hi, [&](int64_t c, float z) {
+        if (c != t) return;
+        if (parts == 1) target = z;
+        else target_z[row] = z;
+    });
+    if (threadIdx.x != 0) return;
     if (parts == 1) write_results(out, g.facts.targets, g.classes, row, s, target);
     else sums[p * g.rows + row] = make_float4(s.m, s.s, s.t, 0.f);
 }
-// dz of such logits: a lane has four neighbouring classes
+// dz of such logits: a lane has four neighbouring classes.  Of a row whose lse is far, every block sums up all of its classes,
+// which the caches hold: a launch less for all calls, where few classes, and so few blocks to a row, are the rule.
 __global__ __launch_bounds__(256) void thin_grads_kernel(ThinRows g, char* dz, int64_t dz_ld, int dz_classes) {
     const unsigned quads = (unsigned)dz_classes / 4, blocks = (quads + 255) / 256;
     const int64_t row = blockIdx.x / blocks;
     const unsigned quad = (blockIdx.x - (unsigned)row * blocks) * 256 + threadIdx.x;
+    LogitGrad grad = logit_grad(g.facts, row, g.classes);
+    if (grad.far) {                    // (the same for the whole block)
+        const float2 far = far_base(thin_row_sums(g, row, 0, g.classes, [](int64_t, float) {}));
+        grad.base = far.x;
+        grad.low = far.y;
+    }
     if (quad >= quads) return;
     const int64_t c = (int64_t)quad * 4;
     float d[4] = {0.f, 0.f, 0.f, 0.f};
     if (c < g.classes) {
         const float4 v = thin_logits(g, row, c);
-        const LogitGrad grad = logit_grad(g.facts, row, g.classes);
         const float z[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) d[e] = c + e < g.classes ? grad.of<false>(z[e], c + e == grad.target) : 0.f;
+        for (int e = 0; e < 4; ++e) d[e] = c + e < g.classes ? grad.of<true>(z[e], c + e == grad.target) : 0.f;
     }
     store_planes(dz + row * dz_ld, c, d);
 }
@@ -667,15 +723,18 @@ __global__ __launch_bounds__(256) void thin_bias_kernel(const char* dz, int64_t 
 
 // ---- joins --------------------------------------------------------------------------------------------------------------
 // The sums of a row's tiles [tile][rows]: a block has ROWS rows, the rest of its threads share their tiles.  32 rows read half a
-// kilobyte at a time; where that leaves few blocks, four.
+// kilobyte at a time; where that leaves few blocks, four.  far: not the results, but, of rows whose lse is far (whose sums alone
+// are there), what dz forms log p from.
 template <int ROWS>
-__global__ __launch_bounds__(256) void classifier_join_kernel(const float4* __restrict__ sums, int64_t tiles, int64_t rows, const int32_t* targets,
-                                                              int64_t classes, const float* target_z, RowResults out) {
+__global__ __launch_bounds__(256) void classifier_join_kernel(const float4* __restrict__ sums, int64_t tiles, int64_t rows, RowFacts facts,
+                                                              int64_t classes, const float* target_z, RowResults out, float2* far) {
     __shared__ float4 part[4][ROWS];
     const int r = threadIdx.x % ROWS, lane = threadIdx.x & 63;
     const int64_t row = (int64_t)blockIdx.x * ROWS + r;
     SoftmaxSums s;
-    if (row < rows) {
+    bool wanted = row < rows;
+    if (far != nullptr && wanted) wanted = row_is_far(facts, row, classes);
+    if (wanted) {
 #pragma unroll 4
         for (int64_t t = threadIdx.x / ROWS; t < tiles; t += 256 / ROWS) {
             const float4 p = sums[t * rows + row];
@@ -696,7 +755,8 @@ __global__ __launch_bounds__(256) void classifier_join_kernel(const float4* __re
         o.m = p.x; o.s = p.y; o.t = p.z;
         softmax_join(s, o);
     }
-    write_results(out, targets, classes, row, s, target_z[row]);      // (without a target: not looked at)
+    if (far == nullptr) write_results(out, facts.targets, classes, row, s, target_z[row]);       // (without a target: not looked at)
+    else if (wanted) far[row] = far_base(s);
 }
 
 // out[r][c] = sum over the slots of part[slot][r][c]: GROUPS of a block's threads share the slots of 256 / GROUPS elements (one:
@@ -846,10 +906,10 @@ struct Plan {
     int thin_parts;
     int64_t thin_part;
     int64_t chunk, chunks;     // of classes, in the backward pass
-    Layout z, dx, dw;
-    int64_t z_tiles;           // of classes (forward), of rows (backward)
+    Layout sums, z, dx, dw;    // sums: z of all classes; z: of a piece of them
+    int64_t sum_tiles, z_tiles;        // of classes; of rows (backward)
     // workspace
-    int64_t x_at, w_at, z_at, sums_at, target_at, dz_at, dz_ld, dx_at, dw_at, db_at, bytes;
+    int64_t x_at, w_at, z_at, sums_at, target_at, far_at, dz_at, dz_ld, dx_at, dw_at, db_at, bytes;
 };
 
 Plan plan_of(int dtype, int64_t rows, int64_t dim, int64_t classes, bool aligned_x, bool aligned_w, bool backward) {
@@ -887,10 +947,10 @@ Plan plan_of(int dtype, int64_t rows, int64_t dim, int64_t classes, bool aligned
         p.thin_parts = (int)ceil_div(classes, p.thin_part);
         p.z_at = take(p.thin_cuts * rows * p.z_ld * 4);
     }
+    p.sums = lay_out(classes, rows, 1, 0);
+    p.sum_tiles = ceil_div(classes, p.sums.big ? kBigTile : kTile);
     if (!backward) {
-        p.z = lay_out(classes, rows, 1, 0);
-        p.z_tiles = ceil_div(classes, p.z.big ? kBigTile : kTile);
-        p.sums_at = take(p.thin ? (p.thin_parts > 1 ? p.thin_parts * rows * 16 : 0) : p.z_tiles * rows * 16);
+        p.sums_at = take(p.thin ? (p.thin_parts > 1 ? p.thin_parts * rows * 16 : 0) : p.sum_tiles * rows * 16);
         p.target_at = take(rows * 4);
     } else {
         const int64_t at_once = std::min(kMostAtOnce, std::max<int64_t>(1, kDzBytes / (rows * 6 * kTile)) * kTile);
@@ -899,7 +959,8 @@ Plan plan_of(int dtype, int64_t rows, int64_t dim, int64_t classes, bool aligned
         p.chunks = ceil_div(classes, p.chunk);
         const int64_t n = std::min(p.chunk, classes);
         p.dz_ld = planes_bytes(n);
-        p.dz_at = take(rows * p.dz_ld);
+        p.far_at = take(p.thin ? 0 : rows * 8);
+        p.dz_at = p.sums_at = take(std::max(rows * p.dz_ld, p.thin ? 0 : p.sum_tiles * rows * 16));       // (the far rows' sums are joined before dz is formed)
         p.z = lay_out(n, rows, 1, 0);
         p.z_tiles = p.thin ? ceil_div(rows, kThinBiasRows) : ceil_div(rows, p.z.big ? kBigTile : kTile);
         p.dx = lay_out(rows, dim, n, kLeastOfGrads);
@@ -946,13 +1007,16 @@ template <typename T> Inputs inputs_of(const ClassifierCall& c, const Plan& p, c
 Operand across(const Operand& o, int64_t rows, int64_t k) { return Operand{o.p, o.ld, rows, k, o.stored}; }
 
 // a by b, `cut` elements of the reduction to a block, on tiles as laid out
-template <Want WANT, int PA, int PB, bool A_ALONG, bool B_ALONG, typename OUT> void launch_gemm(GemmArgs& g, int64_t cut, bool big, hipStream_t st) {
+template <int PA, int PB> void lay_tiles(GemmArgs& g, int64_t cut, bool big) {
     const int64_t side = big ? kBigTile : kTile, KS = big ? Steps<PA, PB, 256>::KS : Steps<PA, PB, 128>::KS;
     g.steps = (int)ceil_div(g.a.k, KS);
     g.steps_per_cut = (int)std::min<int64_t>(g.steps, cut / KS);       // (a cut is a multiple of 64)
     g.tiles_m = (int)ceil_div(g.a.rows, side);
     g.tiles_n = (int)ceil_div(g.b.rows, side);
     g.group = big ? 4 : 8;
+}
+template <Want WANT, int PA, int PB, bool A_ALONG, bool B_ALONG, typename OUT> void launch_gemm(GemmArgs& g, int64_t cut, bool big, hipStream_t st) {
+    lay_tiles<PA, PB>(g, cut, big);
     const dim3 grid((unsigned)(g.tiles_m * g.tiles_n * ceil_div(g.steps, g.steps_per_cut)));
     if (big) hipLaunchKernelGGL((gemm_kernel<WANT, PA, PB, A_ALONG, B_ALONG, OUT, Shape256>), grid, dim3(512), 0, st, g);
     else hipLaunchKernelGGL((gemm_kernel<WANT, PA, PB, A_ALONG, B_ALONG, OUT, Shape128>), grid, dim3(512), 0, st, g);
@@ -986,6 +1050,25 @@ template <typename T> ThinRows thin_forward(const Inputs& in, const float* bias,
     return ThinRows{z, p.z_ld, c.rows, c.classes, p.thin_cuts, bias, facts};
 }
 
+// z on tiles whose sums go to `sums`
+GemmArgs tile_sums(const Inputs& in, const ClassifierCall& c, const RowFacts& facts, float4* sums) {
+    GemmArgs g = {};
+    g.a = in.w;
+    g.b = in.x;
+    g.bias = c.bias;
+    g.classes = g.all_classes = c.classes;
+    g.facts = facts;
+    g.sums = sums;
+    return g;
+}
+void launch_join(const float4* sums, int64_t tiles, const ClassifierCall& c, const RowFacts& facts, const float* target_z, const RowResults& res, float2* far,
+                 hipStream_t st) {
+#define EDL_JOIN(RR) hipLaunchKernelGGL((classifier_join_kernel<RR>), dim3((unsigned)ceil_div(c.rows, RR)), dim3(256), 0, st, sums, tiles, c.rows, facts, c.classes, target_z, res, far)
+    if (c.rows <= kFewRows) EDL_JOIN(4);
+    else EDL_JOIN(32);
+#undef EDL_JOIN
+}
+
 template <typename T> void forward(const ClassifierCall& c, const ClassifierOut& out, hipStream_t st) {
     constexpr int P = sizeof(T) == 2 ? 1 : 3;
     const Plan p = plan_of(c.dtype, c.rows, c.dim, c.classes, lies_aligned(c.x, c.ldx, c.dim, sizeof(T)), lies_aligned(c.w, c.ldw, c.dim, sizeof(T)), false);
@@ -996,7 +1079,7 @@ template <typename T> void forward(const ClassifierCall& c, const ClassifierOut&
     const RowResults res = {out.log_prob, out.entropy, out.lse};
     float4* const sums = (float4*)(work + p.sums_at);
     float* const target_z = (float*)(work + p.target_at);
-    int64_t tiles = p.z_tiles;
+    int64_t tiles = p.sum_tiles;
     if (p.thin) {
         const ThinRows z = thin_forward<T>(in, c.bias, facts, p, c, work, st);
         ProfScope ps("classifier_thin_sums", 0.0, 4.0 * p.thin_cuts * c.rows * c.classes, st);
@@ -1004,22 +1087,13 @@ template <typename T> void forward(const ClassifierCall& c, const ClassifierOut&
         tiles = p.thin_parts;
         if (tiles == 1) return;
     } else {
-        GemmArgs g = {};
-        g.a = in.w;
-        g.b = in.x;
-        g.bias = c.bias;
-        g.classes = c.classes;
-        g.facts = facts;
-        g.sums = sums;
+        GemmArgs g = tile_sums(in, c, facts, sums);
         g.target_z = target_z;
         ProfScope ps("classifier_sums", 2.0 * c.rows * c.classes * c.dim, (double)(c.rows + c.classes) * c.dim * p.esz, st);
-        launch_gemm<SUMS, P, P, true, true, float>(g, kWhole, p.z.big, st);
+        launch_gemm<SUMS, P, P, true, true, float>(g, kWhole, p.sums.big, st);
     }
     ProfScope ps("classifier_join", 0.0, 16.0 * tiles * c.rows, st);
-    if (c.rows <= kFewRows)
-        hipLaunchKernelGGL((classifier_join_kernel<4>), dim3((unsigned)ceil_div(c.rows, 4)), dim3(256), 0, st, sums, tiles, c.rows, c.targets, c.classes, target_z, res);
-    else
-        hipLaunchKernelGGL((classifier_join_kernel<32>), dim3((unsigned)ceil_div(c.rows, 32)), dim3(256), 0, st, sums, tiles, c.rows, c.targets, c.classes, target_z, res);
+    launch_join(sums, tiles, c, facts, target_z, res, nullptr, st);
 }
 
 template <typename OUT> void sum_slots(const float* part, int64_t slots, int64_t rows, int64_t cols, OUT* out, int64_t ld, hipStream_t st) {
@@ -1036,6 +1110,19 @@ template <typename T> void backward(const ClassifierCall& c, const ClassifierGra
     const Inputs in = inputs_of<T>(c, p, work, st);
     const RowFacts facts = {c.targets, d.lse, d.entropy, d.dlog_prob, d.dentropy};
     char* const dz = work + p.dz_at;
+    float2* const far = (float2*)(work + p.far_at);
+    if (!p.thin) {
+        GemmArgs g = tile_sums(in, c, facts, (float4*)(work + p.sums_at));
+        lay_tiles<P, P>(g, kWhole, p.sums.big);
+        {
+            ProfScope ps("classifier_far_sums", 0.0, 0.0, st);
+            const dim3 grid((unsigned)std::min<int64_t>(kChip, (int64_t)g.tiles_m * g.tiles_n));
+            if (p.sums.big) hipLaunchKernelGGL((far_sums_kernel<P, Shape256>), grid, dim3(512), 0, st, g);
+            else hipLaunchKernelGGL((far_sums_kernel<P, Shape128>), grid, dim3(512), 0, st, g);
+        }
+        ProfScope ps("classifier_far_join", 0.0, 0.0, st);
+        launch_join(g.sums, p.sum_tiles, c, facts, nullptr, RowResults{}, far, st);
+    }
     const bool parts_of_dx = p.chunks > 1 || p.dx.cuts > 1;
     for (int64_t q = 0; q < p.chunks; ++q) {
         const int64_t from = q * p.chunk, n = std::min(p.chunk, c.classes - from), cols = round_up(n, 16);
@@ -1062,6 +1149,7 @@ template <typename T> void backward(const ClassifierCall& c, const ClassifierGra
             g.classes = from + n;
             g.all_classes = c.classes;
             g.facts = facts;
+            g.far = far;
             g.dz = dz;
             g.dz_ld = p.dz_ld;
             g.dz_classes = (int)cols;

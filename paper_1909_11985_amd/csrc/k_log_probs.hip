@@ -227,7 +227,7 @@ __device__ __forceinline__ void far_rows_by(const T* logits, T* dlogits, const G
     for (int64_t first = group; first < a.m.rows; first += groups * 64) {
         // (each wave of a block looks at the same 64 rows)
         const int64_t look = first + lane * groups;
-        for (uint64_t left = __ballot(look < a.m.rows && logit_grad(a.facts, min(look, a.m.rows - 1), a.m.cols).far); left != 0; left &= left - 1) {
+        for (uint64_t left = __ballot(look < a.m.rows && row_is_far(a.facts, look, a.m.cols)); left != 0; left &= left - 1) {
             const int64_t row = first + (int64_t)__builtin_ctzll(left) * groups;
             const T* const z = logits + row * a.ld;
             T* const d = dlogits + row * a.ldd;

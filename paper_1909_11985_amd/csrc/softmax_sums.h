@@ -83,6 +83,8 @@ struct LogitGrad {
         return none ? 0.f : hot ? d + g : d;
     }
 };
+// (infinite or not a number: nothing is gained)
+__device__ __forceinline__ bool is_far(float lse) { return fabsf(lse) >= kFarLse && fabsf(lse) < INFINITY; }
 __device__ __forceinline__ LogitGrad logit_grad(const RowFacts& f, int64_t row, int64_t classes) {
     LogitGrad r;
     const int32_t t = f.targets != nullptr ? f.targets[row] : -1;
@@ -94,9 +96,11 @@ __device__ __forceinline__ LogitGrad logit_grad(const RowFacts& f, int64_t row, 
     r.low = 0.f;
     r.both = -(r.g + (r.h != 0.f ? r.h * f.entropy[row] : 0.f));
     r.none = r.g == 0.f && r.h == 0.f;
-    r.far = !r.none && fabsf(r.base) >= kFarLse && fabsf(r.base) < INFINITY;       // (infinite or not a number: as good as it gets)
+    r.far = !r.none && is_far(r.base);
     return r;
 }
+// whether the row is far, by one load where it is not
+__device__ __forceinline__ bool row_is_far(const RowFacts& f, int64_t row, int64_t classes) { return is_far(f.lse[row]) && logit_grad(f, row, classes).far; }
 // what a row that is far takes, from the sums over all of its logits
 __device__ __forceinline__ float2 far_base(const SoftmaxSums& a) { return make_float2(a.m, log2f(a.s) * kLn2); }
 

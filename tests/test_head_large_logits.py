@@ -147,3 +147,83 @@ def test_gradient_of_large_logits_in_a_replayed_graph(E):
         assert torch.equal(held, want), i
         exact, parts, eps = gradient64(z.cpu().double(), t.cpu(), g.cpu(), h.cpu())
         assert bool(((held.cpu().double() - exact).abs() <= parts * (eps + 2.0 ** -24) + 1e-37).all()), i
+
+
+# Features and weights of small whole numbers, so that x w^T is exact, and with it z = x w^T + b for a whole b of up to 2^23;
+# a bias of the type's lowest value takes x w^T in.
+def whole_case(seed, dtype, rows, dim, classes):
+    gen = torch.Generator().manual_seed(seed)
+    x = torch.randint(-1, 2, (rows, dim), generator=gen).to(DT[dtype])
+    w = torch.randint(-1, 2, (classes, dim), generator=gen).to(DT[dtype])
+    t = torch.randint(-1, classes, (rows,), generator=gen, dtype=torch.int32)
+    return x, w, t, gen
+
+
+def check_grads(E, x, w, b, t, z, g, h):
+    """z: the exact logits, in float64; the reference is formed where it lies."""
+    dev, back = (lambda v: v.cuda()), (lambda v: v.to(z.device).double())         # noqa: E731
+    r = E.edl_classifier_log_probs(dev(x), dev(w), dev(b), dev(t))
+    dx, dw, db = E.edl_classifier_log_probs_backward(dev(x), dev(w), dev(b), dev(t), r.lse, r.entropy, dev(g), dev(h))
+    dz, parts, eps = gradient64(z, t.to(z.device), g.to(z.device), h.to(z.device))
+    rows, classes = z.shape
+    xc, wc = back(x), back(w)
+    # dz is stored as three bf16 numbers (2^-24), of which dx of bf16 takes two (2^-16); sums of n float32 terms
+    sums = lambda n: 2.0 ** -24 * (math.sqrt(n) + 8)            # noqa: E731
+    two = 2.0 ** -16 if x.dtype == torch.bfloat16 else 0.0
+    lost = parts * eps
+    want = dz @ wc
+    assert bool(((back(dx) - want).abs() <= lost @ wc.abs() + (parts @ wc.abs()) * (two + sums(classes)) + R.EPS[x.dtype] * want.abs() + 1e-36).all())
+    want = dz.t() @ xc
+    assert bool(((back(dw) - want).abs() <= lost.t() @ xc.abs() + (parts.t() @ xc.abs()) * sums(rows) + 1e-36).all())
+    assert bool(((back(db) - dz.sum(0)).abs() <= lost.sum(0) + parts.sum(0) * sums(rows) + 1e-36).all())
+
+
+WHOLE = [(1, 8, 5), (8, 64, 10), (3, 16, 3000), (31, 40, 24001), (100, 64, 1000), (40, 8, 5000), (5000, 8, 12), (300, 64, 8300), (129, 24, 12500)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("bias", [1e4, -1e5, 1e6, -4e6, "lowest", "half_lowest"])
+@pytest.mark.parametrize("rows,dim,classes", WHOLE)
+def test_classifier_gradients_of_large_logits(E, dtype, bias, rows, dim, classes):
+    x, w, t, gen = whole_case(rows + classes, dtype, rows, dim, classes)
+    lowest = torch.finfo(torch.float32).min
+    z = x.double() @ w.double().t()
+    if isinstance(bias, float):
+        b = bias + torch.randint(-4, 5, (classes,), generator=gen).float()
+        z = z + b.double()
+    else:
+        b = torch.full((classes,), lowest)
+        if bias == "half_lowest":
+            b[1::2] = -math.inf
+        z = b.double().expand(rows, classes).clone()
+    g, h = torch.randn(rows, generator=gen), torch.randn(rows, generator=gen) * 0.3
+    if bias == "half_lowest":
+        t = torch.where((t >= 0) & (t % 2 == 1), t - 1, t)
+    check_grads(E, x, w, b, t, z, g, h)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,dim,classes", WHOLE[1:])
+def test_classifier_gradients_of_some_rows_of_large_logits(E, dtype, rows, dim, classes):
+    """A feature that some rows have lifts all of their logits; the others stay as small as they were."""
+    x, w, t, gen = whole_case(rows * 3 + classes, dtype, rows, dim, classes)
+    x[:, 0] = 0
+    x[::5, 0] = 1
+    w[:, 0] = 131072
+    b = torch.randint(-4, 5, (classes,), generator=gen).float()
+    z = x.double() @ w.double().t() + b.double()
+    g, h = torch.randn(rows, generator=gen), torch.randn(rows, generator=gen) * 0.3
+    check_grads(E, x, w, b, t, z, g, h)       # (131,072 stands in w: dx's first column is a sum of parts as large)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,dim,classes,every", [(1100, 64, 13000, 1), (1100, 64, 13000, 300), (16400, 24, 11003, 1), (16400, 24, 11003, 1000)])
+def test_classifier_gradients_of_large_logits_on_large_tiles_and_in_pieces(E, dtype, rows, dim, classes, every):
+    """256x256 tiles, and more of dz than is held at a time; all rows or few of them have large logits.  The reference is formed on the GPU."""
+    x, w, t, gen = whole_case(rows + every, dtype, rows, dim, classes)
+    x[:, 0] = 0
+    x[every // 2::every, 0] = 1
+    w[:, 0] = -65536
+    b = torch.randint(-4, 5, (classes,), generator=gen).float()
+    z = x.cuda().double() @ w.cuda().double().t() + b.cuda().double()
+    check_grads(E, x, w, b, t, z, torch.randn(rows, generator=gen), torch.randn(rows, generator=gen) * 0.3)
