@@ -281,6 +281,18 @@ def _refuse(msg):
     raise EdlError(-1, msg)
 
 
+def _whole(name, v, least=-2 ** 63, most=2 ** 63 - 1):
+    """v as it is, if the library's type holds it: ctypes would pass what is left of it in that many bits."""
+    if not least <= v <= most:
+        _refuse("%s=%s outside [%d, %d]" % (name, v, least, most))
+    return v
+
+
+def _bits64(name, v):
+    """64 bits, read as a number with or without a sign"""
+    return _whole(name, v, most=2 ** 64 - 1)
+
+
 def _dtype_of(name, x):
     d = x.dtype
     if d is torch.float32:
@@ -330,13 +342,15 @@ def _on(x, stream, work):
 
 def edl_dropout_key(seed, step, layer):
     k = C.c_uint64()
-    _check(lib.edl_dropout_key(seed, step, layer, C.byref(k)))
+    _check(lib.edl_dropout_key(_bits64("seed", seed), _whole("step", step), _whole("layer", layer, -2 ** 31, 2 ** 31 - 1), C.byref(k)))
     return k.value
 
 
 def edl_dropout(x, rate, key, first_row=0, out=None, stream=None):
     """x: [rows][cols] float32 or bfloat16; out: where the result goes (x itself: in place; None: a new tensor).
     The gradient is the same call on the gradient of the result."""
+    _bits64("key", key)
+    _whole("first_row", first_row)
     dt = _dtype_of("x", x)
     px, ldx = _matrix("x", x)
     rows, cols = x.shape
@@ -356,7 +370,7 @@ LogProbs = collections.namedtuple("LogProbs", "log_prob entropy lse top_log_prob
 
 def edl_log_probs_workspace(rows, classes, top=0):
     n = C.c_int64()
-    _check(lib.edl_log_probs_workspace(rows, classes, top, C.byref(n)))
+    _check(lib.edl_log_probs_workspace(_whole("rows", rows), _whole("classes", classes), _whole("top", top, -2 ** 31, 2 ** 31 - 1), C.byref(n)))
     return n.value
 
 
