@@ -266,7 +266,9 @@ def edl_copy(dst, src, nbytes, stream=0):
 # -- operators of a classifier's head ---------------------------------------------------------------------------------
 # Tensors stay where they are: matrices may be views whose rows lie any number of elements apart.  Work goes to torch's
 # current stream of the tensors' device, or to `stream` (a raw stream handle, 0 the default stream); what a call allocates
-# belongs to that stream.  Wrong arguments raise EdlError, as the library's own checks do.  (A small call's time is its host
+# belongs to that stream.  Wrong arguments raise EdlError, as the library's own checks do.  Nothing is recorded for autograd:
+# while it records, tensors that require a gradient are refused (a result without one would lose it); under torch.no_grad(), or
+# in the forward and backward of a torch.autograd.Function, they are taken.  What a call writes to counts as changed.  (A small call's time is its host
 # time, about 4 us of it the launch: the checks below ask for as little as they can.)
 
 def _raw_stream(index):
@@ -293,6 +295,19 @@ def _bits64(name, v):
     return _whole(name, v, most=2 ** 64 - 1)
 
 
+def _recorded(name, v):
+    """Refuses what autograd would have to record."""
+    if v.requires_grad and torch.is_grad_enabled():
+        _refuse("%s requires a gradient, which this call does not record: detach it, call under torch.no_grad() or in a torch.autograd.Function" % name)
+
+
+def _written(*tensors):
+    """Tensors of the caller's (None: not) that a call has written to: autograd must not take them for what it saved."""
+    for v in tensors:
+        if v is not None:
+            torch.autograd.graph.increment_version(v)
+
+
 def _dtype_of(name, x):
     d = x.dtype
     if d is torch.float32:
@@ -304,6 +319,7 @@ def _dtype_of(name, x):
 
 def _matrix(name, x, shape=None, like=None, dtype=None):
     """(pointer, elements between rows) of a [rows][cols] tensor on a GPU (like's, and of its type unless dtype says another)."""
+    _recorded(name, x)
     if x.dim() != 2 or (shape is not None and tuple(x.shape) != shape):
         _refuse("%s must be a matrix%s, not %s" % (name, "" if shape is None else " of %d x %d" % shape, tuple(x.shape)))
     if not x.is_cuda:
@@ -321,6 +337,7 @@ def _vector(name, v, n, dtype, device):
     """Pointer of a contiguous [n] tensor of that type and device; None stays None."""
     if v is None:
         return None
+    _recorded(name, v)
     if v.dtype is not dtype or v.dim() != 1 or v.shape[0] != n or v.device != device or not v.is_contiguous():
         _refuse("%s must be a contiguous %s vector of %d on %s" % (name, dtype, n, device))
     return v.data_ptr()
@@ -359,6 +376,7 @@ def edl_dropout(x, rate, key, first_row=0, out=None, stream=None):
         y = x.new_empty((rows, cols)) if out is None else out
         py, ldy = (y.data_ptr(), cols) if out is None else _matrix("out", out, (rows, cols), x)
         _check(lib.edl_dropout(dt, px, ldx, py, ldy, rows, cols, rate, key, first_row, st))
+        _written(out)
         return y
     return _on(x, stream, work)
 
@@ -418,6 +436,7 @@ def edl_log_probs_backward(logits, targets, lse, entropy, dlog_prob=None, dentro
         d = logits.new_empty((rows, classes)) if out is None else out
         pd, ldd = (d.data_ptr(), classes) if out is None else _matrix("out", out, (rows, classes), logits)
         _check(lib.edl_log_probs_backward(dt, pz, ld, rows, classes, *vec, pd, ldd, st))
+        _written(out)
         return d
     return _on(logits, stream, work)
 
@@ -486,6 +505,7 @@ def edl_classifier_log_probs_backward(x, w, bias, targets, lse, entropy, dlog_pr
         pdx, lddx = _matrix("dx", gx, (rows, dim), x)
         pdw, lddw = _matrix("dw", gw, (classes, dim), x, f32)
         _check(lib.edl_classifier_log_probs_backward(*args, *vec, pdx, lddx, pdw, lddw, _vector("dbias", gb, classes, f32, device), ws, size, st))
+        _written(dx, dw, dbias)
         return gx, gw, gb
     return _on(x, stream, call)
 

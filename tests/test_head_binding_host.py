@@ -32,3 +32,17 @@ def test_numbers_of_alternatives_of_more_bits_are_refused(E):
         with pytest.raises(E.EdlError, match="top|rows|classes") as ei:
             call()
         assert ei.value.code == -1
+
+
+def test_tensors_that_require_a_gradient_are_refused_while_autograd_records(E):
+    x, w = (torch.zeros(*s, requires_grad=True) for s in ((2, 3), (4, 3)))
+    t, f = torch.zeros(2, dtype=torch.int32), torch.zeros(2)
+    calls = [lambda: E.edl_dropout(x, 0.5, 1), lambda: E.edl_log_probs(x), lambda: E.edl_log_probs_backward(x, t, f, f, f), lambda: E.edl_classifier_log_probs(x, w)]
+    for call in calls:
+        with pytest.raises(E.EdlError, match="requires a gradient") as ei:
+            call()
+        assert ei.value.code == -1
+        with torch.no_grad(), pytest.raises(E.EdlError, match="must be on a GPU"):      # (what else is wrong with them)
+            call()
+    with pytest.raises(E.EdlError, match="must be on a GPU"):
+        E.edl_dropout(x.detach(), 0.5, 1)
