@@ -438,14 +438,14 @@ int32_t edl_adam_update(int32_t p, const float* const* dev_grads, const float* s
  * captured into a graph.  Results do not depend on anything but the arguments: no atomics, the same bits every time.
  * Calls of no rows return EDL_OK and touch nothing, unless it says otherwise. */
 
-/* y = kept ? x / (1 - rate) : 0 for a [rows][cols] matrix, rounded once; y may be x (with the same ld) and must not
+/* y = kept ? x s : 0 with s = 1 / (1 - rate) as a float32, for a [rows][cols] matrix, the product rounded once; y may be x (with the same ld) and must not
  * overlap it otherwise.  No mask is stored: whether element (r, c) is kept follows from (key, first_row + r, c) and cols
  * alone, and the gradient of the call is the same call on the gradient of y.  Of row number R = first_row + r, columns 2i
  * and 2i + 1 take the low and the high 32 bits of draw R * ceil(cols/2) + i of the library's generator (SplitMix64, draw j
  * = its finaliser of key + (j+1) * 0x9E3779B97F4A7C15); an element whose 32 bits are below floor(rate * 2^32) is dropped,
  * to +0 whatever it held.  Rows cut differently over calls (by first_row) have the same masks.  Keys of neighbouring
  * values do not give independent masks; edl_dropout_key (host only) makes one from a seed, a step and a layer.
- * EDL_EINVAL: rate outside [0, 1), negative sizes, bad ld or alignment; EDL_ERANGE: rows * ceil(cols/8) over 2^33. */
+ * EDL_EINVAL: rate outside [0, 1), negative sizes, bad ld or alignment; EDL_ERANGE: cols over 2^31 - 1, rows * ceil(cols/8) over 2^33. */
 int32_t edl_dropout_key(uint64_t seed, int64_t step, int32_t layer, uint64_t* out_key);
 int32_t edl_dropout(int32_t dtype, const void* dev_x, int64_t ldx, void* dev_y, int64_t ldy, int64_t rows, int64_t cols, float rate,
                     uint64_t key, int64_t first_row, void* hip_stream);
@@ -462,7 +462,7 @@ int32_t edl_dropout(int32_t dtype, const void* dev_x, int64_t ldx, void* dev_y, 
  * dev_work: edl_log_probs_workspace (host only) bytes, 16-byte aligned; may be NULL if that is 0.  It holds nothing between calls;
  * calls that overlap need one each.
  * EDL_EINVAL: null or misaligned arguments, rows that overlap, classes <= 0, k outside [0, min(64, classes)]; EDL_ENOMEM: workspace
- * too small; EDL_ERANGE: rows over 2^23 or rows * ceil(classes/8) over 2^33. */
+ * too small; EDL_ERANGE: rows over 2^23, classes over 2^31 - 1 or rows * ceil(classes/8) over 2^33. */
 int32_t edl_log_probs_workspace(int64_t rows, int64_t classes, int32_t k, int64_t* out_bytes);
 int32_t edl_log_probs(int32_t dtype, const void* dev_logits, int64_t ld, int64_t rows, int64_t classes, const int32_t* dev_targets, int32_t k,
                       float* dev_log_prob, float* dev_entropy, float* dev_lse, float* dev_top_log_prob, int32_t* dev_top_class,
@@ -497,8 +497,9 @@ int32_t edl_classifier_log_probs(int32_t dtype, const void* dev_x, int64_t ldx, 
 /* Gradients for gradients g = dev_dlog_prob[rows] of log_prob and h = dev_dentropy[rows] of entropy (either may be NULL: zeros):
  * with dz as in edl_log_probs_backward (of rows whose lse is 128 or more away from 0, sums over the classes are formed again), dx = dz w in dtype, dw = dz^T x and dbias = sum of dz over the rows in float32 (what
  * edl_average_update and edl_adam_update take; dev_dbias may be NULL).  The logits are formed again, a piece of the classes at a
- * time, and dz is stored for such a piece (at most 1 GiB of workspace, or 128 classes) as a sum of three bf16 numbers, so that dw and
- * dbias are float32 results.  All outputs are written, not added to, and must not
+ * time, and dz is stored for such a piece as a sum of three bf16 numbers, 6 bytes for each of its logits (1 GiB of workspace at most, or
+ * 128 classes: less than float32 logits would take only where those are over 1 GiB), so that dw and dbias are float32 results; dx of bf16 takes two
+ * of the three (dz to 2^-17) before it is rounded to bf16 (2^-8 at half a step).  All outputs are written, not added to, and must not
  * overlap the inputs (the same address is refused) or each other; of no rows, dw and dbias are zeros.  Arguments and errors as
  * above; the workspace's size is another (backward = 1). */
 int32_t edl_classifier_log_probs_backward(int32_t dtype, const void* dev_x, int64_t ldx, const void* dev_w, int64_t ldw, const float* dev_bias,

@@ -15,8 +15,8 @@
 // so six of them still take less than half of its time.
 //
 // The gradient forms z again rather than keep it, a piece of the classes at a time.  Rows whose lse is far (softmax_sums.h) need
-// their largest logit and sum first: of z in float32 parts, the block that forms their dz sums them up; on tiles the loss's product and join
-// run once more, for the tiles that have such a row alone (5 + 2 us of launches that do nothing where there is none).  dz is stored for the two products that
+// their largest logit and sum first: of z in float32 parts, the block that forms their dz sums them up, or of many classes the loss's sums
+// and join run once more; on tiles its product and join do, for the tiles that have such a row alone (5 + 2 us of launches that do nothing where there is none).  dz is stored for the two products that
 // read it, in both types as three planes: dw is float32, and a single rounding of dz to bf16 would be its largest error by
 // four orders of magnitude.  dx of bf16, which is rounded to bf16 itself, takes the first two.
 //
@@ -655,33 +655,37 @@ template <typename F> __device__ __forceinline__ SoftmaxSums thin_row_sums(const
     }
     return all;
 }
-// Sums of a part of a row's classes; of all of them, the results.
-__global__ __launch_bounds__(256) void thin_sums_kernel(ThinRows g, int parts, int64_t part, float4* sums, float* target_z, RowResults out) {
+// Sums of a part of a row's classes; of all of them, the results.  far_only: the sums alone, of rows whose lse is far.
+__global__ __launch_bounds__(256) void thin_sums_kernel(ThinRows g, int parts, int64_t part, float4* sums, float* target_z, RowResults out, bool far_only) {
     __shared__ float target;
     const int64_t row = blockIdx.x / (unsigned)parts;
+    if (far_only && !row_is_far(g.facts, row, g.classes)) return;
     const int p = (int)(blockIdx.x - (unsigned)row * (unsigned)parts);
     const int64_t lo = p * part, hi = min(lo + part, g.classes);
-    const int64_t t = g.facts.targets != nullptr ? g.facts.targets[row] : -1;
+    const int64_t t = !far_only && g.facts.targets != nullptr ? g.facts.targets[row] : -1;
     const SoftmaxSums s = thin_row_sums(g, row, lo, hi, [&](int64_t c, float z) {
         if (c != t) return;
         if (parts == 1) target = z;
         else target_z[row] = z;
     });
     if (threadIdx.x != 0) return;
-    if (parts == 1) write_results(out, g.facts.targets, g.classes, row, s, target);
+    if (parts == 1 && !far_only) write_results(out, g.facts.targets, g.classes, row, s, target);
     else sums[p * g.rows + row] = make_float4(s.m, s.s, s.t, 0.f);
 }
-// dz of such logits: a lane has four neighbouring classes.  Of a row whose lse is far, every block sums up all of its classes,
-// which the caches hold: a launch less for all calls, where few classes, and so few blocks to a row, are the rule.
-__global__ __launch_bounds__(256) void thin_grads_kernel(ThinRows g, char* dz, int64_t dz_ld, int dz_classes) {
-    const unsigned quads = (unsigned)dz_classes / 4, blocks = (quads + 255) / 256;
+// dz of such logits: a lane has four neighbouring classes.  Of a row whose lse is far, every block sums up all of its classes
+// (launches less for all calls), unless there are more than kFarHere blocks to a row: their sums are then there, joined, in `far`.  (All
+// rows far, 100 x 64 x 24,000 float32: 123 us, 58 where none is; 32 x 64 x 1,000,000: 30 ms by every block, 0.9 from `far`, 0.6.)
+constexpr unsigned kFarHere = 32;
+__host__ __device__ inline unsigned thin_blocks(int64_t quads) { return (unsigned)((quads + 255) / 256); }
+__global__ __launch_bounds__(256) void thin_grads_kernel(ThinRows g, char* dz, int64_t dz_ld, int dz_classes, const float2* far) {
+    const unsigned quads = (unsigned)dz_classes / 4, blocks = thin_blocks(quads);
     const int64_t row = blockIdx.x / blocks;
     const unsigned quad = (blockIdx.x - (unsigned)row * blocks) * 256 + threadIdx.x;
     LogitGrad grad = logit_grad(g.facts, row, g.classes);
     if (grad.far) {                    // (the same for the whole block)
-        const float2 far = far_base(thin_row_sums(g, row, 0, g.classes, [](int64_t, float) {}));
-        grad.base = far.x;
-        grad.low = far.y;
+        const float2 f = far != nullptr ? far[row] : far_base(thin_row_sums(g, row, 0, g.classes, [](int64_t, float) {}));
+        grad.base = f.x;
+        grad.low = f.y;
     }
     if (quad >= quads) return;
     const int64_t c = (int64_t)quad * 4;
@@ -853,7 +857,7 @@ __global__ __launch_bounds__(256) void zero_rows_kernel(float* p, int64_t ld, in
 
 constexpr int64_t kMiB = 1 << 20;
 constexpr int64_t kTile = 128, kBigTile = 256;
-constexpr int64_t kSmallTiles = 192;           // z of fewer 128x128 tiles is formed in parts (thin_logits_kernel)
+constexpr int64_t kSmallTiles = 192;           // z of fewer 128x128 tiles is formed in float32 parts: by thin_logits_kernel up to 32 rows, else by gemm_kernel
 constexpr int64_t kDzBytes = 1024 * kMiB;      // of dz at a time
 constexpr int64_t kZeroAtOnce = 1ll << 30;     // elements of dw that one launch clears where there are no rows
 constexpr int64_t kMostAtOnce = 1 << 20;       // classes of it: offsets in a tile of dz are counted in 31 bits
@@ -905,6 +909,7 @@ struct Plan {
     int64_t z_ld;
     int thin_parts;
     int64_t thin_part;
+    bool far_here;             // dz's blocks sum up the rows whose lse is far
     int64_t chunk, chunks;     // of classes, in the backward pass
     Layout sums, z, dx, dw;    // sums: z of all classes; z: of a piece of them
     int64_t sum_tiles, z_tiles;        // of classes; of rows (backward)
@@ -959,8 +964,10 @@ Plan plan_of(int dtype, int64_t rows, int64_t dim, int64_t classes, bool aligned
         p.chunks = ceil_div(classes, p.chunk);
         const int64_t n = std::min(p.chunk, classes);
         p.dz_ld = planes_bytes(n);
-        p.far_at = take(p.thin ? 0 : rows * 8);
-        p.dz_at = p.sums_at = take(std::max(rows * p.dz_ld, p.thin ? 0 : p.sum_tiles * rows * 16));       // (the far rows' sums are joined before dz is formed)
+        p.far_here = p.thin && thin_blocks(round_up(classes, 16) / 4) <= kFarHere;
+        p.far_at = take(p.far_here ? 0 : rows * 8);
+        // (the far rows' sums are joined before dz is formed)
+        p.dz_at = p.sums_at = take(std::max(rows * p.dz_ld, p.far_here ? 0 : (p.thin ? p.thin_parts : p.sum_tiles) * rows * 16));
         p.z = lay_out(n, rows, 1, 0);
         p.z_tiles = p.thin ? ceil_div(rows, kThinBiasRows) : ceil_div(rows, p.z.big ? kBigTile : kTile);
         p.dx = lay_out(rows, dim, n, kLeastOfGrads);
@@ -1083,7 +1090,7 @@ template <typename T> void forward(const ClassifierCall& c, const ClassifierOut&
     if (p.thin) {
         const ThinRows z = thin_forward<T>(in, c.bias, facts, p, c, work, st);
         ProfScope ps("classifier_thin_sums", 0.0, 4.0 * p.thin_cuts * c.rows * c.classes, st);
-        hipLaunchKernelGGL(thin_sums_kernel, dim3((unsigned)(c.rows * p.thin_parts)), dim3(256), 0, st, z, p.thin_parts, p.thin_part, sums, target_z, res);
+        hipLaunchKernelGGL(thin_sums_kernel, dim3((unsigned)(c.rows * p.thin_parts)), dim3(256), 0, st, z, p.thin_parts, p.thin_part, sums, target_z, res, false);
         tiles = p.thin_parts;
         if (tiles == 1) return;
     } else {
@@ -1132,9 +1139,19 @@ template <typename T> void backward(const ClassifierCall& c, const ClassifierGra
         float* const db = d.dbias == nullptr ? nullptr : p.z_tiles > 1 ? (float*)(work + p.db_at) : d.dbias + from;
         if (p.thin) {
             const ThinRows z = thin_forward<T>(in, c.bias, facts, p, c, work, st);
+            if (!p.far_here) {
+                float4* const sums = (float4*)(work + p.sums_at);
+                {
+                    ProfScope ps("classifier_far_sums", 0.0, 0.0, st);
+                    hipLaunchKernelGGL(thin_sums_kernel, dim3((unsigned)(c.rows * p.thin_parts)), dim3(256), 0, st, z, p.thin_parts, p.thin_part, sums, nullptr, RowResults{}, true);
+                }
+                ProfScope ps("classifier_far_join", 0.0, 0.0, st);
+                launch_join(sums, p.thin_parts, c, facts, nullptr, RowResults{}, far, st);
+            }
             {
                 ProfScope ps("classifier_thin_grads", 0.0, (4.0 * p.thin_cuts + 6.0) * c.rows * c.classes, st);
-                hipLaunchKernelGGL(thin_grads_kernel, dim3((unsigned)(c.rows * ceil_div(cols / 4, 256))), dim3(256), 0, st, z, dz, p.dz_ld, (int)cols);
+                hipLaunchKernelGGL(thin_grads_kernel, dim3((unsigned)(c.rows * thin_blocks(cols / 4))), dim3(256), 0, st, z, dz, p.dz_ld, (int)cols,
+                                   p.far_here ? nullptr : far);
             }
             if (db != nullptr) {
                 ProfScope ps("classifier_thin_bias", 0.0, 6.0 * c.rows * c.classes, st);

@@ -219,7 +219,7 @@ struct GradArgs {
 // lane looks at one row at a time.
 template <typename T, int LANES>
 __device__ __forceinline__ void far_rows_by(const T* logits, T* dlogits, const GradArgs& a, unsigned block) {
-    constexpr int U = 2, WIDE = LANES * kPiece;
+    constexpr int U = 4, WIDE = LANES * kPiece;
     __shared__ float4 wave_sums[4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int me = LANES == 64 ? lane : (int)threadIdx.x;
@@ -231,9 +231,13 @@ __device__ __forceinline__ void far_rows_by(const T* logits, T* dlogits, const G
             const int64_t row = first + (int64_t)__builtin_ctzll(left) * groups;
             const T* const z = logits + row * a.ld;
             T* const d = dlogits + row * a.ldd;
-            SoftmaxSums sums;
-            for (int64_t at = me * kPiece; at < a.m.cols; at += U * WIDE) {
-                float v[U][kPiece], m = sums.m;
+            float v[U][kPiece];
+            auto load = [&](int64_t at) {          // (past the row's end: masked)
+                if (at + (U - 1) * WIDE + kPiece <= a.m.cols) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u) load_piece(z + at + u * WIDE, v[u]);
+                    return;
+                }
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     const int64_t c = at + u * WIDE;
@@ -244,6 +248,11 @@ __device__ __forceinline__ void far_rows_by(const T* logits, T* dlogits, const G
                         for (int e = 0; e < kPiece; ++e) v[u][e] = c + e < a.m.cols ? Elem<T>::to_f32(z[c + e]) : -INFINITY;
                     }
                 }
+            };
+            SoftmaxSums sums;
+            for (int64_t at = me * kPiece; at < a.m.cols; at += U * WIDE) {
+                load(at);
+                float m = sums.m;
 #pragma unroll
                 for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -273,16 +282,20 @@ __device__ __forceinline__ void far_rows_by(const T* logits, T* dlogits, const G
             const float2 far = far_base(sums);
             grad.base = far.x;
             grad.low = far.y;
-            for (int64_t c = me * kPiece; c < a.m.cols; c += WIDE) {
-                const int64_t hot = grad.target - c;
-                if (c + kPiece <= a.m.cols) {
-                    float v[kPiece];
-                    load_piece(z + c, v);
+            for (int64_t at = me * kPiece; at < a.m.cols; at += U * WIDE) {
+                load(at);
 #pragma unroll
-                    for (int e = 0; e < kPiece; ++e) v[e] = grad.template of<true>(v[e], e == hot);
-                    store_piece(d + c, v);
-                } else {
-                    for (int e = 0; c + e < a.m.cols; ++e) d[c + e] = Elem<T>::from_f32(grad.template of<true>(Elem<T>::to_f32(z[c + e]), e == hot));
+                for (int u = 0; u < U; ++u) {
+                    const int64_t c = at + u * WIDE, hot = grad.target - c;
+#pragma unroll
+                    for (int e = 0; e < kPiece; ++e) v[u][e] = grad.template of<true>(v[u][e], e == hot);
+                    if (c + kPiece <= a.m.cols) {
+                        store_piece(d + c, v[u]);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < kPiece; ++e)
+                            if (c + e < a.m.cols) d[c + e] = Elem<T>::from_f32(v[u][e]);
+                    }
                 }
             }
         }

@@ -12,7 +12,8 @@ using namespace edl;
 namespace {
 
 // A launch has fewer than 2^32 work items: element-wise ones have one for up to four pieces of eight elements, others a
-// block of 256 for a row.
+// block of 256 for a row.  kMaxTiles is counted in tiles of 128x128; a block of the classifier's products has 512 threads, but so many
+// tiles are 256x256 ones, a quarter as many, unless one side is at most 1,792 long (longer ones fill them to three quarters): 14 tiles by at most 2^17.
 constexpr int64_t kMaxPieces = 1ll << 33, kMaxRows = 1ll << 23, kMaxDim = 1 << 16, kMaxClasses = 1 << 24, kMaxTiles = 1 << 23;
 
 int launched() {
