@@ -479,7 +479,8 @@ int32_t edl_log_probs_backward(int32_t dtype, const void* dev_logits, int64_t ld
                                const float* dev_lse, const float* dev_entropy, const float* dev_dlog_prob, const float* dev_dentropy,
                                void* dev_dlogits, int64_t ldd, void* hip_stream);
 
-/* edl_log_probs (without alternatives) of the logits x w^T + bias, which are not stored: x [rows][dim] features, w [classes][dim]
+/* edl_log_probs (without alternatives) of the logits x w^T + bias, which the caller never sees (a small call holds float32 parts of them in
+ * the workspace, others only tiles): x [rows][dim] features, w [classes][dim]
  * weights, both in dtype, bias float32 [classes] or NULL; sums in float32.  A bias of -inf masks its class, targets, results and
  * rows at their edges are as there; x and w must be finite.
  * dev_work: edl_classifier_workspace (host only; the pointers are looked at for their alignment only, NULL: any) bytes, 256-byte

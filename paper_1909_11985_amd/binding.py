@@ -474,7 +474,8 @@ def _workspace(args, backward, given, x):
 
 
 def edl_classifier_log_probs(x, w, bias=None, targets=None, work=None, stream=None):
-    """edl_log_probs (without alternatives) of the logits x w^T + bias, which are not stored.  x: [rows][dim], w: [classes][dim]
+    """edl_log_probs (without alternatives) of the logits x w^T + bias without logits in memory (but float32 parts of a small
+    call's, in the workspace).  x: [rows][dim], w: [classes][dim]
     of the same type, bias: float32 [classes].  work: uint8 workspace (None: a new one)."""
     args = _classifier(x, w, bias, targets)
 

@@ -2,8 +2,9 @@
 // gradient of the logits.
 //
 // With the running sums of softmax_sums.h a lane reads each logit once; lanes, waves and parts of a row are then joined.
-// Bound: HBM.  A logit costs about 10 issue slots of full-rate instructions (conversion, maximum, one exponential at a
-// quarter of the rate, two sums), of the 14 that reading bf16 at 5.5 TB/s leaves.
+// Bound: HBM and the vector units together.  A logit costs 9.9 instructions by the counters (conversion, maximum, one exponential at a
+// quarter of the rate, two sums), 13 issue slots of the 14 that reading bf16 at 5.5 TB/s leaves; with the best 10 of 49,999 18.4,
+// whose slots are all of the kernel's time.
 //
 // The best k ride along: after a round of loads only vectors that reach the k-th best of what the wave has seen are put aside
 // in LDS, and their logits then entered into the wave's list, k log(rounds) of them in random order beside the first
@@ -11,7 +12,7 @@
 // for each of a lane's 32 logits: 11 KB of instructions, whose first fetch alone took most of the 13 us of a call for one row.
 //
 // Measured: 4,096 x 49,999 bf16 with 10 alternatives 114 us (3.6 TB/s), 8,192 x 32,768 bf16 without 122 us (4.4 TB/s) and their
-// gradient 216 us (5.0 TB/s) and 5 for the launch that looks for rows whose lse is far (444 in all if every row is); 1 x 32,000 bf16 with 5 in eight parts 8 + 4 us; 256 x 1,000 float32 with 5, a wave to a row, 6 us.
+// gradient 214 us (5.0 TB/s) and 5 for the launch that looks for rows whose lse is far (395 in all if every row is); 1 x 32,000 bf16 with 5 in eight parts 8 + 4 us; 256 x 1,000 float32 with 5, a wave to a row, 6 us.
 #include <algorithm>
 
 #include "operators.h"
